@@ -395,6 +395,88 @@ ff_status ff_train_step_at(const ff_net_desc* net, const ff_net_state* state, co
 size_t ff_workspace_bytes(const ff_net_desc* net);
 
 /* ---------------------------------------------------------------------------------------------
+ * Layer norm and 8-bit activation checkpoints.  For layers with a learned normalisation in front of them, and for gradients
+ * that cross layers: what a backward pass needs is kept in 8 bits and read in that form.
+ *
+ * Matrices of floating-point values in this part
+ *  - [rows, cols], element type `dtype` (FF_F32, FF_BF16 or FF_F16), consecutive columns, rows `ld` ELEMENTS apart,
+ *    ld >= cols; base addresses aligned to the element.  Arithmetic is fp32 whatever the type; results are rounded once.
+ *  - 1 <= cols <= 2^24 and 0 <= rows < 2^31 (FF_ERR_SHAPE / FF_ERR_UNSUPPORTED); no limit at 2^32 elements.
+ *  - rows == 0 is accepted: matrix pointers may be NULL then, sums over rows are zero.
+ *  - An output may be the very matrix of an input of the same shape and type (same base and ld); otherwise they must
+ *    not overlap.
+ *  - Infinities and NaN spread as the formulas say; nothing is skipped or replaced.
+ *
+ * Checkpoints.  A checkpoint of a [rows, cols] matrix is
+ *   q  int8  [rows, ff_pitch(cols)]                   codes in -127 .. 127
+ *   e  uint8 [rows, ff_pitch(ff_ckpt_blocks(cols))]   one exponent byte for every FF_CKPT_BLOCK consecutive columns
+ * both 16-byte aligned, pad bytes zero.  A value is q * 2^(e - 127).  Per block, with a = max|x|: a < 2^-100: codes 0, e = 127; else
+ * e - 127 is the smallest integer s (at most 121) with a <= 127 * 2^s, and q = clamp(round(x * 2^-s), -127, 127), rounded to nearest-even
+ * or stochastically with the random word of ff_quantize for element row*cols+col under (seed, stream_tag).  A block that holds an
+ * infinity or a NaN: codes 0, e = 255, and all its values read as NaN.  Values have at most seven significant bits: they are exact in bf16 and fp32;
+ * read as fp16, those beyond its range are its largest value.
+ * ------------------------------------------------------------------------------------------- */
+enum { FF_F32 = 0, FF_BF16 = 1, FF_F16 = 2 };
+#define FF_CKPT_BLOCK 32
+int64_t ff_ckpt_blocks(int64_t cols);   /* blocks of a row: cols / FF_CKPT_BLOCK rounded up. [host only] */
+
+/* ff_layer_norm_forward — per row: mean = 1/cols sum x, rstd = 1/sqrt(1/cols sum (x - mean)^2 + eps),
+ *   h = (x - mean) * rstd,  y = h * weight + bias
+ *   weight, bias  [cols], type param_dtype (FF_F32 or dtype), either may be NULL (1 and 0)
+ *   mean, rstd    fp32 [rows] (out, either may be NULL)
+ *   q, e          checkpoint of h (out, both or neither): what ff_layer_norm_backward and ff_ckpt_weight_grad read.
+ *                 round_mode, seed and stream_tag are used with it alone. */
+ff_status ff_layer_norm_forward(int64_t rows, int64_t cols, int32_t dtype, int32_t param_dtype, const void* x, int64_t ldx,
+                                const void* weight, const void* bias, float eps, void* y, int64_t ldy, float* mean,
+                                float* rstd, int8_t* q, uint8_t* e, int32_t round_mode, uint64_t seed,
+                                uint64_t stream_tag, void* stream);
+
+/* ff_layer_norm_backward — with g = dy * weight, per row:
+ *   dx = rstd * (g - 1/cols sum g - h * 1/cols sum g h);  dweight = sum over rows of dy h;  dbias = sum over rows of dy
+ *   h comes from x, mean and rstd, or, with x == NULL, from the checkpoint q, e (mean is not read then).
+ *   dx [rows, cols] of type dtype, dweight and dbias fp32 [cols]: any may be NULL, not all three.
+ *   accumulate: 1 adds to dweight and dbias, 0 overwrites them.
+ *   ws: >= ff_layer_norm_workspace_bytes(rows, cols) bytes, 16-byte aligned.
+ * Sums are formed in a fixed order: equal inputs give equal bits. */
+size_t ff_layer_norm_workspace_bytes(int64_t rows, int64_t cols);   /* 0 for sizes that are refused. [host only] */
+ff_status ff_layer_norm_backward(int64_t rows, int64_t cols, int32_t dtype, int32_t param_dtype, const void* dy,
+                                 int64_t lddy, const void* x, int64_t ldx, const float* mean, const int8_t* q,
+                                 const uint8_t* e, const float* rstd, const void* weight, void* dx, int64_t lddx,
+                                 float* dweight, float* dbias, int32_t accumulate, void* ws, size_t ws_bytes,
+                                 void* stream);
+
+/* ff_ckpt_store, ff_ckpt_load — a matrix into a checkpoint, and the values a checkpoint stands for. */
+ff_status ff_ckpt_store(const void* x, int32_t dtype, int64_t ldx, int64_t rows, int64_t cols, int32_t round_mode,
+                        uint64_t seed, uint64_t stream_tag, int8_t* q, uint8_t* e, void* stream);
+ff_status ff_ckpt_load(const int8_t* q, const uint8_t* e, int64_t rows, int64_t cols, void* x, int32_t dtype, int64_t ldx,
+                       void* stream);
+
+/* ff_ckpt_act_backward — gradient through an activation f from the checkpoint of its argument u:
+ *   dx = (dy + 2 * coeff[row] * f(u)) * f'(u)
+ * The second term is the gradient of coeff * G, G = sum f(u)^2 the goodness of the row (ff_goodness_loss gives coeff = dL/dG).
+ * coeff (fp32 [rows]) or dy may be NULL, not both: that term is absent.  f'(0) = 0 for FF_ACT_RELU; FF_ACT_GELU is
+ * u * Phi(u), FF_ACT_SILU u / (1 + exp(-u)). */
+enum { FF_ACT_IDENTITY = 0, FF_ACT_RELU = 1, FF_ACT_GELU = 2, FF_ACT_SILU = 3 };
+ff_status ff_ckpt_act_backward(const int8_t* q, const uint8_t* e, int64_t rows, int64_t cols, int32_t act,
+                               const float* coeff, const void* dy, int64_t lddy, void* dx, int64_t lddx, int32_t dtype,
+                               void* stream);
+
+/* ff_ckpt_weight_grad — weight gradient of a linear layer from the checkpoint of its input, h [rows, k]:
+ *   db[n]    = sum over rows of dy[m][n]
+ *   dw[n][k] = gamma[k] * (sum over rows of dy[m][n] * h[m][k]) + beta[k] * db[n]
+ * With h the normalised row that ff_layer_norm_forward checkpointed and gamma, beta its weight and bias this is the gradient
+ * of the layer behind the norm, whose input gamma * h + beta need not be kept; both NULL: the plain product.
+ *   dy            [rows, n], type dtype, rows lddy elements apart; n <= 65535
+ *   gamma, beta   [k], type param_dtype (FF_F32 or dtype), either may be NULL (1 and 0)
+ *   dw, db        fp32 [n, k] contiguous and [n] (db may be NULL); accumulate as above
+ *   ws            >= ff_ckpt_weight_grad_workspace_bytes(rows, n, k) bytes, 16-byte aligned
+ * Products are exact (dy in up to three bf16 terms against a checkpoint's values), sums fp32 in a fixed order. */
+size_t ff_ckpt_weight_grad_workspace_bytes(int64_t rows, int64_t n, int64_t k);   /* 0 for sizes that are refused. [host only] */
+ff_status ff_ckpt_weight_grad(const void* dy, int32_t dtype, int64_t lddy, const int8_t* q, const uint8_t* e, int64_t rows,
+                              int64_t n, int64_t k, const void* gamma, const void* beta, int32_t param_dtype, float* dw,
+                              float* db, int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Instrumentation (not part of the method).  ff_timing_enable(class_mask): bit c of the mask
  * selects kernel class c (-1 = every class, 0 = off).  Every launch of a selected class is
  * bracketed by a pair of HIP events recorded on the launch stream; ff_timing_read waits for the
@@ -419,7 +501,10 @@ enum {
     FF_K_DWCONV = 10,    /* depthwise convolution: forward and weight gradient */
     FF_K_CHAIN = 11,     /* FF_LOOKAHEAD_CHAIN: gradient combination, its quantisation, input-gradient contraction */
     FF_K_FUSED = 12,     /* the single-launch step of a small dense stack (FF_LAUNCH_FUSED)  */
-    FF_K_COUNT = 13
+    FF_K_NORM = 13,      /* layer norm, forward and backward: one record a call, as for the two below */
+    FF_K_CKPT = 14,      /* 8-bit checkpoints written, read, and read by an activation's gradient */
+    FF_K_CKPT_DW = 15,   /* weight gradient from a checkpoint */
+    FF_K_COUNT = 16
 };
 #define FF_TIMING_MAX_RECORDS 16384
 ff_status ff_timing_enable(int32_t class_mask);

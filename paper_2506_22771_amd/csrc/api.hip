@@ -99,11 +99,6 @@ static ff_status layer_dims(const ff_layer_desc* L, Dims* d)
     return FF_OK;
 }
 
-static bool aligned16(const void* p) { return (((uintptr_t)p) & 15) == 0; }
-static bool aligned4(const void* p) { return (((uintptr_t)p) & 3) == 0; }
-#define HIPCHK(e) do { if ((e) != hipSuccess) return FF_ERR_HIP; } while (0)
-// launch bracketed by timing events of kernel class `cls` on the stream `s` of the enclosing function
-#define HIPCHK_T(cls, e) do { hipError_t _err; { Timed _t((cls), s); _err = (e); } if (_err != hipSuccess) return FF_ERR_HIP; } while (0)
 
 static int32_t goodness_shift(int64_t K, int64_t terms)
 {
@@ -546,33 +541,29 @@ static TimingState g_timing;
 static unsigned long long* g_clock_probe = nullptr;   // device counters of ff_timing_clock_probe (null: off)
 static unsigned long long* g_fused_stamps = nullptr;  // device buffer of ff_timing_fused_stamps (null: off)
 
-struct Timed {
-    hipStream_t s;
-    int idx = -1;
-    Timed(int kernel_class, hipStream_t stream) : s(stream)
-    {
-        TimingState& t = g_timing;
-        if (!((t.mask >> kernel_class) & 1u) || t.n >= FF_TIMING_MAX_RECORDS) return;
-        hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;   // no event records into a graph under capture
-        if (hipStreamIsCapturing(s, &cap) != hipSuccess || cap != hipStreamCaptureStatusNone) return;
-        if (!t.ev) {
-            t.ev = new hipEvent_t[2 * FF_TIMING_MAX_RECORDS];
-            t.cls = new int8_t[FF_TIMING_MAX_RECORDS];
-        }
-        while (t.created <= t.n) {
-            if (hipEventCreate(&t.ev[2 * t.created]) != hipSuccess) return;
-            if (hipEventCreate(&t.ev[2 * t.created + 1]) != hipSuccess) return;
-            ++t.created;
-        }
-        idx = t.n++;
-        t.cls[idx] = (int8_t)kernel_class;
-        (void)hipEventRecord(t.ev[2 * idx], s);
+Timed::Timed(int kernel_class, hipStream_t stream) : s(stream)
+{
+    TimingState& t = g_timing;
+    if (!((t.mask >> kernel_class) & 1u) || t.n >= FF_TIMING_MAX_RECORDS) return;
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;   // no event records into a graph under capture
+    if (hipStreamIsCapturing(s, &cap) != hipSuccess || cap != hipStreamCaptureStatusNone) return;
+    if (!t.ev) {
+        t.ev = new hipEvent_t[2 * FF_TIMING_MAX_RECORDS];
+        t.cls = new int8_t[FF_TIMING_MAX_RECORDS];
     }
-    ~Timed()
-    {
-        if (idx >= 0) (void)hipEventRecord(g_timing.ev[2 * idx + 1], s);
+    while (t.created <= t.n) {
+        if (hipEventCreate(&t.ev[2 * t.created]) != hipSuccess) return;
+        if (hipEventCreate(&t.ev[2 * t.created + 1]) != hipSuccess) return;
+        ++t.created;
     }
-};
+    idx = t.n++;
+    t.cls[idx] = (int8_t)kernel_class;
+    (void)hipEventRecord(t.ev[2 * idx], s);
+}
+Timed::~Timed()
+{
+    if (idx >= 0) (void)hipEventRecord(g_timing.ev[2 * idx + 1], s);
+}
 
 static Im2colArgs im2col_args(const Dims& d, const int8_t* aq, int64_t st_aq, int8_t* col, int64_t st_col, int nb)
 {

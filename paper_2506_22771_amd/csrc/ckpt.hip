@@ -1,0 +1,269 @@
+// 8-bit checkpoints of activations: written, read back, and read by the gradient through an activation function.
+//
+//   store:         q, e = codes and exponent bytes of x (ckpt.hpp)            load:  x = q 2^(e - 127)
+//   act backward:  dx = (dy + 2 c[row] f(u)) f'(u), u the checkpointed argument of f; 2 c f(u) is the gradient of c G, the goodness
+//                  G = sum f(u)^2 of Section III (dL/dG = c), dy what comes down from the layers above (either may be absent)
+//
+// All three are bound by memory.  A lane has eight columns (a chunk) of a row, a quad of lanes one block; a workgroup takes consecutive chunks,
+// whatever the row length, and has all its loads in flight before the first is used.
+#include <math.h>
+
+#include "ckpt.hpp"
+#include "norm.hpp"
+
+namespace ffi {
+
+constexpr int CK_THREADS = 256;
+
+// Consecutive chunks of a matrix; rows are `slots` chunks long (a multiple of four, so that quads hold blocks).
+struct Chunks {
+    int64_t total;
+    uint32_t slots, magic;   // magic: ceil(2^32 / slots)
+};
+static Chunks chunks_of(int64_t rows, int64_t bytes_or_cols)
+{
+    const int64_t slots = (bytes_or_cols + 31) / 32 * 4;
+    return {rows * slots, (uint32_t)slots, (uint32_t)(((uint64_t(1) << 32) + (uint64_t)slots - 1) / (uint64_t)slots)};
+}
+// Row and chunk of `at` chunks (fewer than 4096) behind the workgroup's first one, (row0, chunk0).  Rows of 4096 chunks or more: at most one row
+// further; shorter ones: at + chunk0 < 8192, where the product with the rounded-up reciprocal has the quotient exactly.
+__device__ __forceinline__ void chunk_place(const Chunks& c, int64_t row0, uint32_t chunk0, uint32_t at, int64_t& row, uint32_t& chunk)
+{
+    const uint32_t o = chunk0 + at;
+    const uint32_t r = c.slots >= 4096u ? (o >= c.slots ? 1u : 0u) : __umulhi(o, c.magic);
+    row = row0 + r;
+    chunk = o - r * c.slots;
+}
+__device__ __forceinline__ void chunk_first(const Chunks& c, int64_t first, int64_t& row0, uint32_t& chunk0)
+{
+    if (first >> 32) {
+        row0 = first / c.slots;
+        chunk0 = (uint32_t)(first - row0 * c.slots);
+    } else {
+        const uint32_t r = (uint32_t)first / c.slots;
+        row0 = r;
+        chunk0 = (uint32_t)first - r * c.slots;
+    }
+}
+
+template <typename T> struct CkptArgs {
+    Chunks c;
+    CkptPtr k;
+    CkptRound r;
+    const T* in;       // store: x; act backward: dy (may be null)
+    T* out;            // load: x; act backward: dx
+    int64_t ld_in, ld_out;
+    const float* coeff;   // act backward: may be null
+    int32_t cols, act;
+};
+
+template <typename T, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckpt_store(CkptArgs<T> a)
+{
+    const int64_t first = (int64_t)blockIdx.x * (CK_THREADS * U);
+    int64_t row0;
+    uint32_t chunk0;
+    chunk_first(a.c, first, row0, chunk0);
+    Raw8<T> raw[U];
+    int64_t row[U];
+    uint32_t chunk[U];
+    int n[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const uint32_t at = i * CK_THREADS + threadIdx.x;
+        chunk_place(a.c, row0, chunk0, at, row[i], chunk[i]);
+        n[i] = first + at < a.c.total ? min(8, a.cols - 8 * (int)chunk[i]) : 0;   // (at most 0: no columns of x)
+        raw[i] = load_raw(a.in + row[i] * a.ld_in + 8 * chunk[i], max(0, n[i]));
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        float v[8];
+        raw_values(raw[i], v);
+        const uint32_t m = quad_max_u32(abs_max_bits(v)), e = ckpt_exponent(m);
+        const u32x2 q = ckpt_codes(v, m, e, a.r, (uint64_t)row[i] * (uint64_t)a.cols + 8 * (uint64_t)chunk[i]);
+        if (first + i * CK_THREADS + threadIdx.x < a.c.total) ckpt_store_chunk(a.k, row[i], (int)chunk[i], (int)a.c.slots, n[i] > 0, q, e);
+    }
+}
+
+// A code rounded up can stand for more than fp16 holds (65504 becomes 64 * 2^10): given as the largest value.
+template <typename T> __device__ __forceinline__ float ckpt_clamp(float v) { return v; }
+template <> __device__ __forceinline__ float ckpt_clamp<f16_t>(float v) { return v == v ? __builtin_amdgcn_fmed3f(v, -65504.0f, 65504.0f) : v; }
+
+template <typename T, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckpt_load(CkptArgs<T> a)
+{
+    const int64_t first = (int64_t)blockIdx.x * (CK_THREADS * U);
+    int64_t row0;
+    uint32_t chunk0;
+    chunk_first(a.c, first, row0, chunk0);
+    u32x2 q[U];
+    uint32_t e[U];
+    T* to[U];
+    int n[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const uint32_t at = i * CK_THREADS + threadIdx.x;
+        int64_t row;
+        uint32_t chunk;
+        chunk_place(a.c, row0, chunk0, at, row, chunk);
+        n[i] = first + at < a.c.total ? min(8, a.cols - 8 * (int)chunk) : 0;
+        to[i] = a.out + row * a.ld_out + 8 * chunk;
+        q[i] = u32x2{0, 0};
+        e[i] = 127;
+        if (n[i] > 0) {
+            q[i] = *(const u32x2*)(a.k.q + row * a.k.pitch + 8 * chunk);
+            e[i] = a.k.e[row * a.k.epitch + (chunk >> 2)];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        float v[8];
+        ckpt_values(q[i], e[i], v);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = ckpt_clamp<T>(v[u]);
+        if (n[i] > 0) store8(to[i], n[i], v);
+    }
+}
+
+// f(u) and f'(u).
+template <int ACT> __device__ __forceinline__ void act_of(float u, float& f, float& d)
+{
+    if constexpr (ACT == FF_ACT_RELU) {
+        f = u > 0 ? u : (u == u ? 0.0f : u);
+        d = u > 0 ? 1.0f : (u == u ? 0.0f : u);
+    } else if constexpr (ACT == FF_ACT_GELU) {
+        const float phi = 0.5f * (1.0f + erff(u * 0.70710678118654752f));
+        f = u * phi;
+        d = __builtin_fmaf(u * 0.39894228040143268f, expf(-0.5f * u * u), phi);
+    } else if constexpr (ACT == FF_ACT_SILU) {
+        const float sig = 1.0f / (1.0f + expf(-u));
+        f = u * sig;
+        d = sig * (1.0f + u * (1.0f - sig));
+    } else {
+        f = u;
+        d = 1.0f;
+    }
+}
+
+template <typename T, int ACT, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckpt_act_backward(CkptArgs<T> a)
+{
+    const int64_t first = (int64_t)blockIdx.x * (CK_THREADS * U);
+    int64_t row0;
+    uint32_t chunk0;
+    chunk_first(a.c, first, row0, chunk0);
+    Raw8<T> raw[U];
+    u32x2 q[U];
+    uint32_t e[U];
+    float c2[U];
+    T* to[U];
+    int n[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const uint32_t at = i * CK_THREADS + threadIdx.x;
+        int64_t row;
+        uint32_t chunk;
+        chunk_place(a.c, row0, chunk0, at, row, chunk);
+        n[i] = first + at < a.c.total ? min(8, a.cols - 8 * (int)chunk) : 0;
+        to[i] = a.out + row * a.ld_out + 8 * chunk;
+        raw_zero(raw[i]);
+        q[i] = u32x2{0, 0};
+        e[i] = 127;
+        c2[i] = 0;
+        if (n[i] > 0) {
+            if (a.in) raw[i] = load_raw(a.in + row * a.ld_in + 8 * chunk, n[i]);
+            q[i] = *(const u32x2*)(a.k.q + row * a.k.pitch + 8 * chunk);
+            e[i] = a.k.e[row * a.k.epitch + (chunk >> 2)];
+            if (a.coeff) c2[i] = 2.0f * a.coeff[row];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        float u[8], v[8];
+        ckpt_values(q[i], e[i], u);
+        raw_values(raw[i], v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float f, d;
+            act_of<ACT>(u[j], f, d);
+            v[j] = (a.coeff ? __builtin_fmaf(c2[i], f, v[j]) : v[j]) * d;
+        }
+        if (n[i] > 0) store8(to[i], n[i], v);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// launches
+// ------------------------------------------------------------------------------------------------
+template <typename T> static CkptArgs<T> ckpt_args(const int8_t* q, const uint8_t* e, int64_t rows, int64_t cols, int64_t span)
+{
+    CkptArgs<T> a = {};
+    a.c = chunks_of(rows, span);
+    a.k = ckpt_ptr(q, e, cols);
+    a.cols = (int32_t)cols;
+    return a;
+}
+template <int U> static unsigned ckpt_grid(const Chunks& c) { return (unsigned)((c.total + CK_THREADS * U - 1) / (CK_THREADS * U)); }
+
+template <typename T> static hipError_t store_of(const void* x, int64_t ldx, int64_t rows, int64_t cols, const CkptRound& r, int8_t* q, uint8_t* e, hipStream_t s)
+{
+    CkptArgs<T> a = ckpt_args<T>(q, e, rows, cols, pitch8(cols));   // pad columns are written too
+    a.in = (const T*)x;
+    a.ld_in = ldx;
+    a.r = r;
+    k_ckpt_store<T, 2><<<ckpt_grid<2>(a.c), CK_THREADS, 0, s>>>(a);
+    return hipGetLastError();
+}
+hipError_t launch_ckpt_store(const void* x, int32_t dtype, int64_t ldx, int64_t rows, int64_t cols, int32_t round_mode, uint64_t seed,
+                             uint64_t tag, int8_t* q, uint8_t* e, hipStream_t s)
+{
+    if (rows == 0) return hipSuccess;
+    const CkptRound r = {make_sr_key(seed, tag), round_mode == FF_ROUND_STOCHASTIC};
+    return dtype == FF_F32    ? store_of<float>(x, ldx, rows, cols, r, q, e, s)
+           : dtype == FF_BF16 ? store_of<bf16_t>(x, ldx, rows, cols, r, q, e, s)
+                              : store_of<f16_t>(x, ldx, rows, cols, r, q, e, s);
+}
+
+template <typename T> static hipError_t load_of(const int8_t* q, const uint8_t* e, int64_t rows, int64_t cols, void* x, int64_t ldx, hipStream_t s)
+{
+    CkptArgs<T> a = ckpt_args<T>(q, e, rows, cols, cols);
+    a.out = (T*)x;
+    a.ld_out = ldx;
+    k_ckpt_load<T, 2><<<ckpt_grid<2>(a.c), CK_THREADS, 0, s>>>(a);
+    return hipGetLastError();
+}
+hipError_t launch_ckpt_load(const int8_t* q, const uint8_t* e, int64_t rows, int64_t cols, void* x, int32_t dtype, int64_t ldx,
+                            hipStream_t s)
+{
+    if (rows == 0) return hipSuccess;
+    return dtype == FF_F32    ? load_of<float>(q, e, rows, cols, x, ldx, s)
+           : dtype == FF_BF16 ? load_of<bf16_t>(q, e, rows, cols, x, ldx, s)
+                              : load_of<f16_t>(q, e, rows, cols, x, ldx, s);
+}
+
+template <typename T>
+static hipError_t act_backward_of(const int8_t* q, const uint8_t* e, int64_t rows, int64_t cols, int32_t act, const float* coeff, const void* dy,
+                                  int64_t lddy, void* dx, int64_t lddx, hipStream_t s)
+{
+    CkptArgs<T> a = ckpt_args<T>(q, e, rows, cols, cols);
+    a.in = (const T*)dy;
+    a.ld_in = lddy;
+    a.out = (T*)dx;
+    a.ld_out = lddx;
+    a.coeff = coeff;
+    const unsigned grid = ckpt_grid<2>(a.c);
+    switch (act) {
+        case FF_ACT_RELU: k_ckpt_act_backward<T, FF_ACT_RELU, 2><<<grid, CK_THREADS, 0, s>>>(a); break;
+        case FF_ACT_GELU: k_ckpt_act_backward<T, FF_ACT_GELU, 2><<<grid, CK_THREADS, 0, s>>>(a); break;
+        case FF_ACT_SILU: k_ckpt_act_backward<T, FF_ACT_SILU, 2><<<grid, CK_THREADS, 0, s>>>(a); break;
+        default: k_ckpt_act_backward<T, FF_ACT_IDENTITY, 2><<<grid, CK_THREADS, 0, s>>>(a); break;
+    }
+    return hipGetLastError();
+}
+hipError_t launch_ckpt_act_backward(const int8_t* q, const uint8_t* e, int64_t rows, int64_t cols, int32_t act, const float* coeff,
+                                    const void* dy, int64_t lddy, void* dx, int64_t lddx, int32_t dtype, hipStream_t s)
+{
+    if (rows == 0) return hipSuccess;
+    return dtype == FF_F32    ? act_backward_of<float>(q, e, rows, cols, act, coeff, dy, lddy, dx, lddx, s)
+           : dtype == FF_BF16 ? act_backward_of<bf16_t>(q, e, rows, cols, act, coeff, dy, lddy, dx, lddx, s)
+                              : act_backward_of<f16_t>(q, e, rows, cols, act, coeff, dy, lddy, dx, lddx, s);
+}
+
+}  // namespace ffi

@@ -1,0 +1,441 @@
+// Weight gradient of a linear layer from the 8-bit checkpoint of its input:
+//
+//     dW[n][k] = gamma[k] S[n][k] + beta[k] db[n],   S[n][k] = sum over rows m of dy[m][n] x[m][k],   db[n] = sum over rows m of dy[m][n]
+//
+// x is what the checkpoint stands for.  Behind a layer norm that is the normalised row h, and gamma, beta are the norm's parameters: the layer's
+// input gamma h + beta is never kept, its share of the gradient follows from the two sums.
+//
+// The products run on bf16 matrix instructions with fp32 accumulators.  A checkpoint's value q 2^s is exact in bf16.  dy is taken as one (bf16), two
+// (fp16) or three (fp32) bf16 terms, split by truncation, so that their sum is dy exactly (what lies below 2^-126 aside) and every product is exact: the only
+// roundings are those of the fp32 sums, as in a product of fp32 matrices, of which this is several times the rate.
+//
+// A workgroup of four wavefronts owns BT x BT outputs and walks over the rows in steps of BM.  Both operands lie in memory with the reduction (m)
+// as the slow axis.  A step's BM x BT elements go through registers, which is where codes become bf16 and dy its terms, into LDS as
+// they lie, and the fragments are read with the transposing LDS read.  Three stages of LDS: while a step is multiplied the one after the next is
+// written and the first fragments of the next are read already, so that no wavefront waits for LDS behind the barrier; registers hold the step after those.
+#include <type_traits>
+
+#include "ckpt.hpp"
+#include "norm.hpp"
+
+namespace ffi {
+
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+constexpr int WG_T = 256;   // threads: two by two wavefronts
+
+template <typename T> struct Terms;
+template <> struct Terms<bf16_t> { static constexpr int N = 1; };
+template <> struct Terms<f16_t> { static constexpr int N = 2; };
+template <> struct Terms<float> { static constexpr int N = 3; };
+// Rows of a step: three stages of all terms and the checkpoint's values in LDS, which two workgroups share where tiles are small.
+template <typename T, int BT> constexpr int step_rows() { return Terms<T>::N == 3 && BT > 64 ? 16 : 32; }
+
+struct WgradArgs {
+    const void* dy;
+    int64_t lddy;
+    CkptPtr c;
+    int64_t rows;
+    int32_t n, k, tiles_n, tiles_k, splits;
+    int64_t steps, per;      // steps of all rows, steps of a split
+    int64_t plain;           // steps before this one are read without looking at the end of the matrix
+    const void* gamma;
+    const void* beta;
+    int32_t param_kind;      // type of gamma and beta
+    float* dw;
+    float* db;
+    int32_t accumulate;
+    float* part;             // splits > 1: [splits][n][k], then [splits][n]
+};
+
+__device__ __forceinline__ float param_at(const void* p, int kind, int64_t at, float none)
+{
+    if (!p) return none;
+    if (kind == FF_F32) return ((const float*)p)[at];
+    const uint32_t w = ((const uint16_t*)p)[at];
+    return kind == FF_BF16 ? bf16_value(w) : (float)__builtin_bit_cast(_Float16, (uint16_t)w);
+}
+
+// Transposing LDS read of 16-bit elements: each group of 16 lanes reads four rows of 32 bytes (lanes 4r .. 4r + 3 give the
+// quarters of row r) and lane j of the group receives column j, rows 0 .. 3.
+__device__ __forceinline__ v4s tr_read16(const char* p)
+{
+    typedef __attribute__((address_space(3))) v4s* lds_ptr;
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)p);
+}
+// Chunk (16 bytes, eight elements) c of row m lies at c ^ swizzle(m): the eight rows of 64 bytes that one transposing read of a wavefront takes
+// then fall into different banks.
+template <int BT> __device__ __forceinline__ int swizzle(int m)
+{
+    return BT == 256 ? ((m & 3) | ((m >> 1) & 4)) << 2 : BT == 128 ? (m & 3) << 2 : ((m >> 1) & 1) << 2;
+}
+
+// The bf16 terms of eight values of dy: t0 + t1 + t2, each the leading bits of what the ones before leave (truncated, which is exact: 24 bits are three
+// times eight).  Infinities stay in the first term alone; a NaN is one in one of the terms.
+__device__ __forceinline__ void terms_of(const Raw8<bf16_t>& r, u32x4 t[1]) { t[0] = r.a; }
+__device__ __forceinline__ uint32_t high_pair(float lo, float hi) { return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u); }
+__device__ __forceinline__ float rest_of(float v)
+{
+    const float lead = __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);
+    return __builtin_fabsf(v) == __builtin_inff() ? 0.0f : v - lead;
+}
+__device__ __forceinline__ void terms_of(const Raw8<f16_t>& r, u32x4 t[2])
+{
+    float v[8];
+    raw_values(r, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        t[0][i] = high_pair(v[2 * i], v[2 * i + 1]);
+        t[1][i] = high_pair(rest_of(v[2 * i]), rest_of(v[2 * i + 1]));
+    }
+}
+__device__ __forceinline__ void terms_of(const Raw8<float>& r, u32x4 t[3])
+{
+    float v[8];
+    raw_values(r, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float a = v[2 * i], b = v[2 * i + 1], a1 = rest_of(a), b1 = rest_of(b);
+        t[0][i] = high_pair(a, b);
+        t[1][i] = high_pair(a1, b1);
+        t[2][i] = high_pair(rest_of(a1), rest_of(b1));
+    }
+}
+
+// v + the sum of eight bf16 values
+__device__ __forceinline__ float sum_of(v8bf f, float v)
+{
+    const v2bf one = {(__bf16)1.0f, (__bf16)1.0f};
+    v = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(f, f, 0, 1), one, v, false);
+    v = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(f, f, 2, 3), one, v, false);
+    v = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(f, f, 4, 5), one, v, false);
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(f, f, 6, 7), one, v, false);
+}
+
+template <typename T, int BT> struct WgradTile {
+    static constexpr int P = Terms<T>::N, BM = step_rows<T, BT>();
+    static constexpr int CPR = BT / 8;                   // chunks of a row
+    static constexpr int CH = BM * CPR / WG_T;           // chunks of a thread, of each operand
+    static constexpr int ROWS = WG_T / CPR;              // rows between a thread's chunks
+    static constexpr int PLANE = BM * BT * 2;            // bytes of one term
+    static constexpr int STAGE = (P + 1) * PLANE;
+    static constexpr int SUB = BM / 16;                  // matrix instructions along a step
+    static constexpr int WT = BT / 2, TI = WT / 32;      // a wavefront's outputs, in tiles of 32
+    static constexpr int PIECES = SUB * P * TI;          // a wavefront's fragments of dy in a step, TI matrix instructions each
+    static constexpr int LDS = 3 * STAGE;
+    static_assert(CH >= 1 && LDS <= 160 * 1024 && ROWS % 8 == 0 && PIECES % CH == 0, "tile");
+};
+
+template <typename T, int BT>
+__global__ __launch_bounds__(WG_T) __attribute__((amdgpu_waves_per_eu(BT == 256 ? 1 : 2))) void k_ckpt_wgrad(WgradArgs a)
+{
+    using S = WgradTile<T, BT>;
+    __shared__ __attribute__((aligned(16))) char lds[S::LDS];
+    const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, lh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wn = wave >> 1, wk = wave & 1;
+    // Workgroups go to the eight XCDs in turn: each takes consecutive tiles, in bands of four tiles of n, so that its L2 holds few panels.
+    const int items = a.tiles_n * a.tiles_k * a.splits, per_xcd = (items + 7) >> 3;
+    const int item = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
+    if (item >= items) return;   // (uniform)
+    const int tiles = a.tiles_n * a.tiles_k, split = item / tiles, tile = item - split * tiles;
+    const int band = tile / (4 * a.tiles_k), in_band = tile - band * 4 * a.tiles_k, height = min(4, a.tiles_n - 4 * band);
+    const int tk = in_band / height, tn = 4 * band + in_band - tk * height;
+    const int n0 = tn * BT, k0 = tk * BT;
+    const int64_t step0 = split * a.per, step1 = min(step0 + a.per, a.steps);
+
+    // This thread's chunk column, and rows r0, r0 + ROWS, ...  Columns that do not exist are read as some that do: their outputs are not stored.
+    const int cc = tid % S::CPR, r0 = tid / S::CPR;
+    const int cn = min(n0 + 8 * cc, (a.n - 1) & ~7);
+    const int64_t ck = min((int64_t)(k0 + 8 * cc), a.c.pitch - 8);
+    const int cb = min((k0 + 8 * cc) >> 5, a.c.blocks - 1);
+    const T* const dy = (const T*)a.dy + cn;
+    const int8_t* const cq = a.c.q + ck;
+    const uint8_t* const ce = a.c.e + cb;
+    struct Chunk { Raw8<T> d; u32x2 q; uint32_t e; };
+    // A chunk of dy may reach into the next row (n not a multiple of eight); that stays inside the matrix but for the last row.
+    auto fetch = [&](int64_t step, int i) {
+        const int64_t m = step * S::BM + r0 + i * S::ROWS;
+        return Chunk{load_raw(dy + m * a.lddy, 8), *(const u32x2*)(cq + m * a.c.pitch), ce[m * a.c.epitch]};
+    };
+    // Rows that do not exist are zero in both operands, columns beyond n too.
+    auto fetch_last = [&](int64_t step, int i) {
+        const int64_t m = step * S::BM + r0 + i * S::ROWS;
+        Chunk c = {{}, {0, 0}, 0};
+        if (m < a.rows) c = Chunk{load_raw(dy + m * a.lddy, min(8, a.n - cn)), *(const u32x2*)(cq + m * a.c.pitch), ce[m * a.c.epitch]};
+        return c;
+    };
+    auto put = [&](char* stage, int i, const Chunk& c) {
+        const int m = r0 + i * S::ROWS;
+        char* const at = stage + m * (BT * 2) + ((cc ^ swizzle<BT>(m)) << 4);
+        u32x4 t[S::P];
+        terms_of(c.d, t);
+#pragma unroll
+        for (int p = 0; p < S::P; ++p) *(u32x4*)(at + p * S::PLANE) = t[p];
+        float v[8];
+        ckpt_values(c.q, c.e, v);
+        u32x4 x;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = high_pair(v[2 * u], v[2 * u + 1]);   // (exact)
+        *(u32x4*)(at + S::P * S::PLANE) = x;
+    };
+
+    v16f acc[S::TI][S::TI];
+    float db[S::TI];
+#pragma unroll
+    for (int i = 0; i < S::TI; ++i) {
+        db[i] = 0;
+#pragma unroll
+        for (int j = 0; j < S::TI; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0;
+    }
+    // A lane's place in a transposing read: row 8 lh + (lane & 15) / 4 of a 16-row piece (and four rows on for the second half of a fragment, where
+    // the swizzle is the same), columns 16 ((lane >> 4) & 1) + 4 (lane & 3) of a 32-column tile.
+    const int tr_row = 8 * lh + ((lane & 15) >> 2), tr_at = tr_row * (BT * 2) + ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) << 4) + 8 * (lane & 1);
+    int at_n[S::TI], at_k[S::TI];
+#pragma unroll
+    for (int i = 0; i < S::TI; ++i) {
+        at_n[i] = tr_at + ((((wn * S::WT + 32 * i) >> 3) ^ swizzle<BT>(tr_row)) << 4);
+        at_k[i] = tr_at + ((((wk * S::WT + 32 * i) >> 3) ^ swizzle<BT>(tr_row)) << 4) + S::P * S::PLANE;
+    }
+    auto fragment = [&](const char* stage, int at, int more) {   // more: a constant
+        const v4s lo = tr_read16(stage + at + more), hi = tr_read16(stage + at + more + 4 * BT * 2);
+        return __builtin_bit_cast(v8bf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto fragment_n = [&](const char* stage, int piece) {
+        const int i = piece % S::TI, p = piece / S::TI % S::P, s = piece / (S::TI * S::P);
+        return fragment(stage, at_n[i], s * 16 * BT * 2 + p * S::PLANE);
+    };
+    auto meet = [&] {   // this wavefront's LDS operations are done, then everybody's; loads from memory stay on their way
+        wait_lds();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    const int64_t plain = min(step1, a.plain);   // steps read without looking at the end
+    if (step0 < plain) {
+        Chunk c[S::CH];
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+#pragma unroll
+            for (int i = 0; i < S::CH; ++i) c[i] = fetch(min(step0 + st, plain - 1), i);
+#pragma unroll
+            for (int i = 0; i < S::CH; ++i) put(lds + st * S::STAGE, i, c[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < S::CH; ++i) c[i] = fetch(min(step0 + 2, plain - 1), i);
+        meet();
+        char *now = lds, *next = lds + S::STAGE, *after = lds + 2 * S::STAGE;
+        v8bf fa = fragment_n(now, 0), fb[S::TI];
+#pragma unroll
+        for (int j = 0; j < S::TI; ++j) fb[j] = fragment(now, at_k[j], 0);
+        for (int64_t step = step0; step < plain; ++step) {
+            const int64_t ahead = min(step + 3, plain - 1);   // (behind the last step: the last one again, which nobody uses)
+            float sum[S::TI];
+#pragma unroll
+            for (int i = 0; i < S::TI; ++i) sum[i] = 0;
+            v8bf fb_next[S::TI];
+#pragma unroll
+            for (int piece = 0; piece < S::PIECES; ++piece) {
+                const int i = piece % S::TI, s = piece / (S::TI * S::P);
+                const bool last_of_sub = (piece + S::TI) / (S::TI * S::P) > s;   // the last term's pieces: the next fragments of k are read
+                const v8bf fa_next = piece + 1 < S::PIECES ? fragment_n(now, piece + 1) : fragment_n(next, 0);
+                if (last_of_sub) fb_next[i] = s + 1 < S::SUB ? fragment(now, at_k[i], (s + 1) * 16 * BT * 2) : fragment(next, at_k[i], 0);
+#pragma unroll
+                for (int j = 0; j < S::TI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
+                sum[i] = sum_of(fa, sum[i]);
+                constexpr int EVERY = S::PIECES / S::CH;
+                if (piece % EVERY == 0) {
+                    put(after, piece / EVERY, c[piece / EVERY]);
+                    c[piece / EVERY] = fetch(ahead, piece / EVERY);
+                }
+                fa = fa_next;
+                if (last_of_sub && i == S::TI - 1) {
+#pragma unroll
+                    for (int j = 0; j < S::TI; ++j) fb[j] = fb_next[j];
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int i = 0; i < S::TI; ++i) db[i] += sum[i];
+            meet();
+            char* const first = now;
+            now = next;
+            next = after;
+            after = first;
+        }
+    }
+    // what is left: the step with the last row, or all of them where a chunk may reach over several rows (n < 8)
+    for (int64_t step = max(step0, plain); step < step1; ++step) {
+        meet();
+#pragma nounroll
+        for (int i = 0; i < S::CH; ++i) put(lds, i, fetch_last(step, i));
+        meet();
+#pragma nounroll
+        for (int s = 0; s < S::SUB; ++s) {
+            v8bf fb[S::TI];
+#pragma unroll
+            for (int j = 0; j < S::TI; ++j) fb[j] = fragment(lds + s * 16 * BT * 2, at_k[j], 0);
+#pragma unroll
+            for (int piece = 0; piece < S::P * S::TI; ++piece) {
+                const int i = piece % S::TI;
+                const v8bf fa = fragment_n(lds + s * 16 * BT * 2, piece);
+#pragma unroll
+                for (int j = 0; j < S::TI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
+                db[i] = sum_of(fa, db[i]);
+            }
+        }
+    }
+    meet();
+
+    // sums of dy, which both wavefronts of a half of n have: the halves of a wavefront, through LDS (which nothing reads any more)
+    float* const sums = (float*)lds;
+#pragma unroll
+    for (int i = 0; i < S::TI; ++i) {
+        const float both = db[i] + __shfl_xor(db[i], 32);
+        if (lh == 0 && wk == 0) sums[wn * S::WT + 32 * i + lr] = both;
+    }
+    __syncthreads();
+    const bool whole = a.splits == 1;
+    float* const out = whole ? a.dw : a.part + (int64_t)split * a.n * a.k;
+    if (tk == 0)
+        for (int i = tid; i < BT && n0 + i < a.n; i += WG_T) {
+            const float v = sums[i];
+            if (!whole) a.part[(int64_t)a.splits * a.n * a.k + (int64_t)split * a.n + n0 + i] = v;
+            else if (a.db) a.db[n0 + i] = a.accumulate ? a.db[n0 + i] + v : v;
+        }
+#pragma unroll
+    for (int j = 0; j < S::TI; ++j) {
+        const int k = k0 + wk * S::WT + 32 * j + lr;
+        if (k >= a.k) continue;
+        const float g = whole ? param_at(a.gamma, a.param_kind, k, 1.0f) : 1.0f, b = whole ? param_at(a.beta, a.param_kind, k, 0.0f) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < S::TI; ++i)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int nl = wn * S::WT + 32 * i + (v & 3) + 8 * (v >> 2) + 4 * lh, n = n0 + nl;
+                if (n >= a.n) continue;
+                float r = acc[i][j][v];
+                float* const to = out + (int64_t)n * a.k + k;
+                if (whole) {
+                    r = g * r;
+                    if (a.beta) r = __builtin_fmaf(b, sums[nl], r);
+                    if (a.accumulate) r += *to;
+                }
+                *to = r;
+            }
+    }
+}
+
+// Adds the splits' partial sums, in order, and applies gamma and beta.  No splits (no rows): zero.
+__global__ __launch_bounds__(256) void k_ckpt_wgrad_sum(WgradArgs a)
+{
+    const float* const pdb = a.part + (int64_t)a.splits * a.n * a.k;
+    const int64_t size = (int64_t)a.n * a.k;
+    const int n = blockIdx.y;
+    float d = 0;
+    if (a.beta || a.db)
+        for (int s = 0; s < a.splits; ++s) d += pdb[(int64_t)s * a.n + n];
+    if (a.db && blockIdx.x == 0 && threadIdx.x == 0) a.db[n] = a.accumulate ? a.db[n] + d : d;
+    const int k = (int)(blockIdx.x * 256 + threadIdx.x);
+    if (k >= a.k) return;
+    const int64_t at = (int64_t)n * a.k + k;
+    float v = 0;
+#pragma unroll 8
+    for (int s = 0; s < a.splits; ++s) v += a.part[s * size + at];
+    v = param_at(a.gamma, a.param_kind, k, 1.0f) * v;
+    if (a.beta) v = __builtin_fmaf(param_at(a.beta, a.param_kind, k, 0.0f), d, v);
+    a.dw[at] = a.accumulate ? a.dw[at] + v : v;
+}
+
+// ------------------------------------------------------------------------------------------------
+// launches
+// ------------------------------------------------------------------------------------------------
+struct WgradPlan {
+    int tile, splits;
+    int64_t steps, per;
+};
+static int plan_rows(int terms, int tile) { return terms == 3 && tile > 64 ? 16 : 32; }
+// Tile and split of the rows.
+static WgradPlan wgrad_plan(int64_t rows, int64_t n, int64_t k, int terms)
+{
+    WgradPlan best = {64, 1, 0, 0};
+    double least = 0;
+    const int tiles[3] = {256, 128, 64};
+    for (int i = 0; i < 3; ++i) {
+        const int bt = tiles[i], bm = plan_rows(terms, bt);
+        const int64_t count = ((n + bt - 1) / bt) * ((k + bt - 1) / bt), steps = (rows + bm - 1) / bm;
+        for (int64_t s = 1; s <= 256 && s <= (steps > 0 ? steps : 1); s *= 2) {
+            if (s > 1 && s * n * k > (int64_t(1) << 26)) break;
+            const int64_t per = (steps + s - 1) / s, real = per > 0 ? (steps + per - 1) / per : 1;
+            const int slots = 256 * (bt == 256 ? 1 : 2);   // workgroups that run at once
+            const double rounds = (double)((count * real + slots - 1) / slots);
+            // microseconds: a step's products at the rate its tile reaches, what starts and ends a workgroup, and the sum of the splits
+            const double rate = bt == 256 ? 4.2e6 : bt == 128 ? 1.6e6 : 0.6e6;   // multiply-adds per microsecond and workgroup
+            const double t = rounds * (3.0 + (double)per * bm * bt * bt * terms / rate) + (real > 1 ? 3.0 + (double)real * n * k * 8e-6 / 4.5 : 0.0);
+            if (least == 0 || t < least) {
+                least = t;
+                best = {bt, (int)real, steps, per};
+            }
+        }
+    }
+    return best;
+}
+size_t ckpt_wgrad_workspace(int64_t rows, int64_t n, int64_t k)
+{
+    size_t most = FF_WS_MIN_BYTES;
+    for (int terms = 1; terms <= 3; ++terms) {
+        const WgradPlan p = wgrad_plan(rows, n, k, terms);
+        const size_t need = p.splits > 1 ? align_up((size_t)p.splits * (size_t)(n * k + n) * sizeof(float), 256) : 0;
+        if (need > most) most = need;
+    }
+    return most;
+}
+
+template <typename T> static hipError_t wgrad_of(const CkptWgradLaunch& l, hipStream_t s)
+{
+    const WgradPlan p = wgrad_plan(l.rows, l.n, l.k, Terms<T>::N);
+    WgradArgs a;
+    a.dy = l.dy;
+    a.lddy = l.lddy;
+    a.c = ckpt_ptr(l.q, l.e, l.k);
+    a.rows = l.rows;
+    a.n = (int32_t)l.n;
+    a.k = (int32_t)l.k;
+    a.tiles_n = (int32_t)((l.n + p.tile - 1) / p.tile);
+    a.tiles_k = (int32_t)((l.k + p.tile - 1) / p.tile);
+    a.splits = l.rows > 0 ? p.splits : 0;
+    a.steps = p.steps;
+    a.per = p.per;
+    const int bm = plan_rows(Terms<T>::N, p.tile);
+    a.plain = l.n < 8 ? 0 : l.rows % bm == 0 && l.n % 8 == 0 ? p.steps : p.steps - 1;
+    a.gamma = l.gamma;
+    a.beta = l.beta;
+    a.param_kind = l.param_dtype;
+    a.dw = l.dw;
+    a.db = l.db;
+    a.accumulate = l.accumulate;
+    a.part = (float*)l.ws;
+    if (l.rows > 0) {
+        const unsigned grid = (unsigned)(((int64_t)a.tiles_n * a.tiles_k * a.splits + 7) / 8 * 8);
+        if (p.tile == 256) k_ckpt_wgrad<T, 256><<<grid, WG_T, 0, s>>>(a);
+        else if (p.tile == 128) k_ckpt_wgrad<T, 128><<<grid, WG_T, 0, s>>>(a);
+        else k_ckpt_wgrad<T, 64><<<grid, WG_T, 0, s>>>(a);
+        const hipError_t err = hipGetLastError();
+        if (err != hipSuccess) return err;
+    }
+    if (a.splits != 1) {
+        k_ckpt_wgrad_sum<<<dim3((unsigned)((a.k + 255) / 256), (unsigned)a.n), 256, 0, s>>>(a);
+        return hipGetLastError();
+    }
+    return hipSuccess;
+}
+hipError_t launch_ckpt_wgrad(const CkptWgradLaunch& a, hipStream_t s)
+{
+    return a.dtype == FF_F32 ? wgrad_of<float>(a, s) : a.dtype == FF_BF16 ? wgrad_of<bf16_t>(a, s) : wgrad_of<f16_t>(a, s);
+}
+
+}  // namespace ffi

@@ -22,6 +22,19 @@ __host__ __device__ static inline int64_t pitch8(int64_t cols)
 __host__ __device__ static inline int64_t pitch32(int64_t cols) { return (cols + 3) & ~int64_t(3); }
 static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
+// ---- entry points -----------------------------------------------------------------------------
+static inline bool aligned16(const void* p) { return (((uintptr_t)p) & 15) == 0; }
+static inline bool aligned4(const void* p) { return (((uintptr_t)p) & 3) == 0; }
+struct Timed {   // timing events of one kernel class around what runs in its scope (api.hip)
+    hipStream_t s;
+    int idx = -1;
+    Timed(int kernel_class, hipStream_t stream);
+    ~Timed();
+};
+#define HIPCHK(e) do { if ((e) != hipSuccess) return FF_ERR_HIP; } while (0)
+// launch bracketed by timing events of kernel class `cls` on the stream `s` of the enclosing function
+#define HIPCHK_T(cls, e) do { hipError_t _err; { Timed _t((cls), s); _err = (e); } if (_err != hipSuccess) return FF_ERR_HIP; } while (0)
+
 // ---- stochastic-rounding key (Section IV-B cites stochastic rounding; the generator is ours) --
 struct SrKey {
     uint32_t k0;  // low word of the 64-bit key

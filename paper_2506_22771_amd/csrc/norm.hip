@@ -1,0 +1,567 @@
+// Layer norm, forward and backward, over the rows of a matrix of fp32, bf16 or fp16 values.
+//
+//   mean = 1/C sum x,  rstd = 1 / sqrt(1/C sum (x - mean)^2 + eps),  h = (x - mean) rstd,  y = h w + b
+//   g = dy w,  dx = rstd (g - 1/C sum g - h 1/C sum g h),  dw = sum over rows of dy h,  db = sum over rows of dy
+//
+// Statistics, products and sums are fp32; y and dx are rounded once.  The variance is summed around the mean, in a second pass over values
+// that are held in registers, so a row far from zero loses nothing.
+//
+// Both are bound by memory: a row is read once and held in registers by a group of 4 to 1024 lanes, eight columns (a chunk) of a lane
+// at a time.  The forward pass can write the checkpoint of h beside y, and the backward pass reads h from it (1.03 bytes a value) instead of x.
+#include <type_traits>
+
+#include "ckpt.hpp"
+#include "norm.hpp"
+
+namespace ffi {
+
+template <int LANES> struct Group {
+    static constexpr int THREADS = LANES <= 64 ? 256 : LANES;
+    static constexpr int ROWS = THREADS / LANES;   // groups of a workgroup
+};
+
+// Sum over the lanes of a group, which every lane receives.  Groups of more than a wavefront meet in `red`, one word per wavefront
+// and sum, which the caller does not use twice between barriers.
+template <int LANES, int N> __device__ __forceinline__ void group_sum(float (&v)[N], float* red)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        auto add = [&](auto ctrl) { v[i] += __uint_as_float(dpp_u32<decltype(ctrl)::value>(__float_as_uint(v[i]))); };
+        add(std::integral_constant<int, 0xB1>());                                  // quad_perm [1,0,3,2]
+        add(std::integral_constant<int, 0x4E>());                                  // quad_perm [2,3,0,1]
+        if constexpr (LANES >= 8) add(std::integral_constant<int, 0x141>());       // row_half_mirror
+        if constexpr (LANES >= 16) add(std::integral_constant<int, 0x140>());      // row_mirror
+        if constexpr (LANES >= 32) v[i] += __shfl_xor(v[i], 16);
+        if constexpr (LANES >= 64) v[i] += __shfl_xor(v[i], 32);
+    }
+    if constexpr (LANES > 64) {
+        constexpr int W = LANES / 64;
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) red[i * W + wave] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float t = 0;
+#pragma unroll
+            for (int w = 0; w < W; ++w) t += red[i * W + w];
+            v[i] = t;
+        }
+    }
+}
+
+// Eight parameters of a chunk (n of them exist), in the element's type or in fp32; `none` where there are none.
+template <typename T> __device__ __forceinline__ void load_param(const void* p, bool f32, int64_t at, int n, float none, float v[8])
+{
+    if (p == nullptr) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = none;
+    } else if (sizeof(T) == 4 || f32) {
+        load8((const float*)p + at, n, v);
+    } else {
+        load8((const T*)p + at, n, v);
+    }
+}
+
+template <typename T> struct NormForwardArgs {
+    const T* x;
+    T* y;
+    int64_t ldx, ldy, rows;
+    const void* weight;
+    const void* bias;
+    float* mean;
+    float* rstd;
+    int32_t cols, param_f32;
+    float eps, inv_cols;
+    CkptPtr k;
+    CkptRound r;
+};
+
+// CH chunks of a lane; CH == 0: any number, read three times (rows beyond 32768 columns, which the caches hold).
+template <typename T, int LANES, int CH>
+__global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForwardArgs<T> a)
+{
+    constexpr int W = LANES > 64 ? LANES / 64 : 1;
+    __shared__ float red[2][W];
+    const int j = threadIdx.x % LANES;
+    const int64_t row_at = (int64_t)blockIdx.x * Group<LANES>::ROWS + threadIdx.x / LANES;
+    const bool there = row_at < a.rows;
+    const int64_t row = there ? row_at : a.rows - 1;   // (lanes of a row that does not exist go along and store nothing)
+    const T* const x = a.x + row * a.ldx;
+    T* const y = a.y + row * a.ldy;
+    constexpr int UNROLL = CH ? CH : 1;
+    const int chunks = CH ? CH : (int)((a.k.pitch / 8 + LANES - 1) / LANES);
+    float v[CH ? CH : 1][8];
+    Raw8<T> raw[CH ? CH : 1];
+    auto count = [&](int c) { return max(0, min(8, a.cols - 8 * c)); };
+    if constexpr (CH != 0) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int c = j + i * LANES, n = count(c);
+            raw[i] = load_raw(x + 8 * c, n);
+        }
+#pragma unroll
+        for (int i = 0; i < CH; ++i) raw_values(raw[i], v[i]);
+    }
+    auto values = [&](int i, int n) {   // CH == 0: the chunk is read again
+        if (CH == 0) load8(x + 8 * (j + i * LANES), n, v[0]);
+        return CH ? i : 0;
+    };
+    float sum[1] = {0};
+#pragma unroll UNROLL
+    for (int i = 0; i < chunks; ++i) {
+        const int at = values(i, count(j + i * LANES));
+#pragma unroll
+        for (int u = 0; u < 8; ++u) sum[0] += v[at][u];
+    }
+    group_sum<LANES, 1>(sum, red[0]);
+    const float mean = sum[0] * a.inv_cols;
+    // columns that do not exist lie at the mean from here on
+    auto pad = [&](int at, int n) {
+        if (n < 8) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[at][u] = u < n ? v[at][u] : mean;
+        }
+    };
+    sum[0] = 0;
+#pragma unroll UNROLL
+    for (int i = 0; i < chunks; ++i) {
+        const int n = count(j + i * LANES), at = values(i, n);
+        pad(at, n);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const float d = v[at][u] - mean;
+            sum[0] = __builtin_fmaf(d, d, sum[0]);
+        }
+    }
+    group_sum<LANES, 1>(sum, red[1]);
+    const float rstd = 1.0f / sqrtf(sum[0] * a.inv_cols + a.eps);
+    if (there && j == 0) {
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+#pragma unroll UNROLL
+    for (int i = 0; i < chunks; ++i) {
+        const int c = j + i * LANES, n = count(c), at = values(i, n);
+        if (CH == 0) pad(at, n);
+        float h[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) h[u] = (v[at][u] - mean) * rstd;
+        if (n > 0) {
+            float w[8], b[8], o[8];
+            load_param<T>(a.weight, a.param_f32, 8 * c, n, 1.0f, w);
+            load_param<T>(a.bias, a.param_f32, 8 * c, n, 0.0f, b);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) o[u] = __builtin_fmaf(h[u], w[u], b[u]);
+            if (there) store8(y + 8 * c, n, o);
+        }
+        if (a.k.q) {
+            const uint32_t m = quad_max_u32(abs_max_bits(h)), e = ckpt_exponent(m);
+            const u32x2 q = ckpt_codes(h, m, e, a.r, (uint64_t)row * (uint64_t)a.cols + 8 * (uint64_t)c);
+            if (there) ckpt_store_chunk(a.k, row, c, LANES * chunks, n > 0, q, e);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// Backward.  A workgroup keeps the column sums of its rows in registers (a lane's columns never change) and leaves them in the
+// workspace; k_norm_columns adds the workgroups' sums in order, so results do not depend on timing.
+// ------------------------------------------------------------------------------------------------
+template <typename T> struct NormBackwardArgs {
+    const T* dy;
+    const T* x;
+    T* dx;
+    int64_t lddy, ldx, lddx, rows;
+    const float* mean;
+    const float* rstd;
+    const void* weight;
+    int32_t cols, param_f32, sums;   // sums: dweight or dbias is wanted
+    float inv_cols;
+    CkptPtr k;
+    float* part;        // [workgroups][2][pcols]
+    int64_t pcols;
+    float2* row_sums;   // rows too wide for registers: both means of every row
+};
+
+// Values that the compiler is not to trace back: it would keep what it made of them before instead of making it again, which takes more registers
+// than there are.
+__device__ __forceinline__ void opaque(u32x4& v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void opaque(u32x2& v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void opaque(Raw8<float>& r) { opaque(r.a); opaque(r.b); }
+__device__ __forceinline__ void opaque(Raw8<bf16_t>& r) { opaque(r.a); }
+__device__ __forceinline__ void opaque(Raw8<f16_t>& r) { opaque(r.a); }
+
+// Rows a group has in flight.
+template <typename T, int CH> constexpr int rows_ahead() { return (sizeof(T) == 4 ? 2 : 4) / CH; }
+
+template <typename T, bool KEPT, int LANES, int CH>
+__global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_backward(NormBackwardArgs<T> a)
+{
+    using G = Group<LANES>;
+    constexpr int W = LANES > 64 ? LANES / 64 : 1, R = rows_ahead<T, CH>();
+    __shared__ float red[2][2 * R * W];
+    __shared__ __attribute__((aligned(16))) float cols_lds[G::ROWS > 1 ? G::THREADS * 16 : 4];
+    const int j = threadIdx.x % LANES, group = threadIdx.x / LANES;
+    const int64_t groups = (int64_t)gridDim.x * G::ROWS, g0 = (int64_t)blockIdx.x * G::ROWS + group;
+    auto count = [&](int i) { return max(0, min(8, a.cols - 8 * (j + i * LANES))); };
+    float w[CH][8], dw[CH][8], db[CH][8];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u) dw[i][u] = db[i][u] = 0;
+        load_param<T>(a.weight, a.param_f32, 8 * (j + i * LANES), count(i), 1.0f, w[i]);
+    }
+    int phase = 0;
+    // every group of a workgroup of several wavefronts makes the same number of rounds: barriers are inside
+    const int64_t rounds = (a.rows + groups * R - 1) / (groups * R);
+    for (int64_t it = 0; it < rounds; ++it, phase ^= 1) {
+        Raw8<T> rd[R][CH];
+        std::conditional_t<KEPT, u32x2, Raw8<T>> rx[R][CH];
+        uint32_t re[R][CH];
+        float mean[R], rstd[R];
+        int64_t row[R];
+        bool there[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            row[k] = (it * R + k) * groups + g0;
+            there[k] = row[k] < a.rows;
+            if (!there[k]) row[k] = a.rows - 1;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int c = j + i * LANES, n = there[k] ? count(i) : 0;
+                re[k][i] = 127;
+                if constexpr (KEPT) {
+                    rx[k][i] = u32x2{0, 0};
+                    if (n > 0) {
+                        rx[k][i] = *(const u32x2*)(a.k.q + row[k] * a.k.pitch + 8 * c);
+                        re[k][i] = a.k.e[row[k] * a.k.epitch + (c >> 2)];
+                    }
+                } else {
+                    rx[k][i] = load_raw(a.x + row[k] * a.ldx + 8 * c, n);
+                }
+                rd[k][i] = load_raw(a.dy + row[k] * a.lddy + 8 * c, n);
+            }
+            // (a row that does not exist adds zeros, whatever the last row holds)
+            rstd[k] = there[k] ? a.rstd[row[k]] : 0.0f;
+            mean[k] = KEPT || !there[k] ? 0.0f : a.mean[row[k]];
+        }
+        auto rows_values = [&](int k, int i, float d[8], float h[8]) {
+            raw_values(rd[k][i], d);
+            if constexpr (KEPT) {
+                ckpt_values(rx[k][i], re[k][i], h);
+            } else {
+                raw_values(rx[k][i], h);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) h[u] = (h[u] - mean[k]) * rstd[k];
+            }
+        };
+        float s[2 * R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            s[2 * k] = s[2 * k + 1] = 0;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                // (a column that does not exist has d = 0 and adds nothing, or a NaN where the row's own columns have them too)
+                float d[8], h[8];
+                rows_values(k, i, d, h);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const float g = d[u] * w[i][u];
+                    s[2 * k] += g;
+                    s[2 * k + 1] = __builtin_fmaf(g, h[u], s[2 * k + 1]);
+                    dw[i][u] = __builtin_fmaf(d[u], h[u], dw[i][u]);
+                    db[i][u] += d[u];
+                }
+            }
+        }
+        if (a.dx) {
+            group_sum<LANES, 2 * R>(s, red[phase]);
+#pragma unroll
+            for (int k = 0; k < R; ++k)
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    opaque(rd[k][i]);
+                    opaque(rx[k][i]);
+                }
+#pragma unroll
+            for (int k = 0; k < R; ++k) {
+                const float c1 = s[2 * k] * a.inv_cols, c2 = s[2 * k + 1] * a.inv_cols;
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    const int c = j + i * LANES, n = there[k] ? count(i) : 0;
+                    float d[8], h[8];
+                    rows_values(k, i, d, h);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) d[u] = rstd[k] * (d[u] * w[i][u] - c1 - h[u] * c2);
+                    store8(a.dx + row[k] * a.lddx + 8 * c, n, d);
+                }
+            }
+        }
+    }
+    if (!a.sums) return;
+    float* const out = a.part + (int64_t)blockIdx.x * 2 * a.pcols;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const int c = j + i * LANES;
+        if constexpr (G::ROWS > 1) {   // the workgroup's groups hold the same columns: sixteen words a lane, added in order
+            float* const mine = cols_lds + threadIdx.x * 16;
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                mine[u] = dw[i][u];
+                mine[8 + u] = db[i][u];
+            }
+            __syncthreads();
+            for (int t = threadIdx.x; t < LANES * 16; t += G::THREADS) {
+                float v = 0;
+#pragma unroll 4
+                for (int g = 0; g < G::ROWS; ++g) v += cols_lds[g * LANES * 16 + t];
+                const int64_t col = 8 * (int64_t)(t / 16 + i * LANES) + (t & 7);
+                if (col < a.pcols) out[((t >> 3) & 1) * a.pcols + col] = v;
+            }
+        } else if (8 * c < a.pcols) {
+#pragma unroll
+            for (int u = 0; u < 8; u += 4) {
+                *(float4*)(out + 8 * c + u) = make_float4(dw[i][u], dw[i][u + 1], dw[i][u + 2], dw[i][u + 3]);
+                *(float4*)(out + a.pcols + 8 * c + u) = make_float4(db[i][u], db[i][u + 1], db[i][u + 2], db[i][u + 3]);
+            }
+        }
+    }
+}
+
+// Rows of more columns than a workgroup holds: their two means first, ...
+template <typename T, bool KEPT> __global__ __launch_bounds__(1024) void k_norm_row_sums(NormBackwardArgs<T> a)
+{
+    __shared__ float red[2 * 16];
+    const int64_t row = blockIdx.x;
+    float s[2] = {0, 0};
+    const float rstd = a.rstd[row], mean = KEPT ? 0.0f : a.mean[row];
+    for (int c = threadIdx.x; 8 * c < a.cols; c += 1024) {
+        const int n = min(8, a.cols - 8 * c);
+        float d[8], h[8], w[8];
+        load8(a.dy + row * a.lddy + 8 * c, n, d);
+        if constexpr (KEPT) {
+            ckpt_values(*(const u32x2*)(a.k.q + row * a.k.pitch + 8 * c), a.k.e[row * a.k.epitch + (c >> 2)], h);
+        } else {
+            load8(a.x + row * a.ldx + 8 * c, n, h);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) h[u] = (h[u] - mean) * rstd;
+        }
+        load_param<T>(a.weight, a.param_f32, 8 * c, n, 1.0f, w);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const float g = d[u] * w[u];
+            s[0] += g;
+            s[1] = __builtin_fmaf(g, h[u], s[1]);
+        }
+    }
+    group_sum<1024, 2>(s, red);
+    if (threadIdx.x == 0) a.row_sums[row] = make_float2(s[0] * a.inv_cols, s[1] * a.inv_cols);
+}
+// ... then dx and the column sums of 2048 columns and every gridDim.y-th row.
+template <typename T, bool KEPT> __global__ __launch_bounds__(256) void k_norm_backward_wide(NormBackwardArgs<T> a)
+{
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    const int n = min(8, a.cols - 8 * c);
+    if (n <= 0) return;
+    float w[8], dw[8], db[8];
+    load_param<T>(a.weight, a.param_f32, 8 * c, n, 1.0f, w);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) dw[u] = db[u] = 0;
+    for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+        const float rstd = a.rstd[row], mean = KEPT ? 0.0f : a.mean[row];
+        float d[8], h[8];
+        load8(a.dy + row * a.lddy + 8 * c, n, d);
+        if constexpr (KEPT) {
+            ckpt_values(*(const u32x2*)(a.k.q + row * a.k.pitch + 8 * c), a.k.e[row * a.k.epitch + (c >> 2)], h);
+        } else {
+            load8(a.x + row * a.ldx + 8 * c, n, h);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) h[u] = (h[u] - mean) * rstd;
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            dw[u] = __builtin_fmaf(d[u], h[u], dw[u]);
+            db[u] += d[u];
+        }
+        if (a.dx) {
+            const float2 m = a.row_sums[row];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) d[u] = rstd * (d[u] * w[u] - m.x - h[u] * m.y);
+            store8(a.dx + row * a.lddx + 8 * c, n, d);
+        }
+    }
+    if (!a.sums) return;
+    float* const out = a.part + (int64_t)blockIdx.y * 2 * a.pcols + 8 * c;   // (pcols is a multiple of eight)
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        out[u] = dw[u];
+        out[a.pcols + u] = db[u];
+    }
+}
+
+// Adds the workgroups' column sums: 16 columns by 16 slices of the workgroups, then the slices in order.
+__global__ __launch_bounds__(256) void k_norm_columns(const float* part, int parts, int64_t pcols, int cols, float* dw, float* db,
+                                                      int accumulate)
+{
+    __shared__ float red[16][17];
+    const int col = blockIdx.x * 16 + (threadIdx.x & 15), slice = threadIdx.x >> 4;
+    float* const out = blockIdx.y ? db : dw;
+    if (!out) return;
+    float v = 0;
+    if (col < cols) {
+        const float* const p = part + blockIdx.y * pcols + col;
+#pragma unroll 8
+        for (int g = slice; g < parts; g += 16) v += p[(int64_t)g * 2 * pcols];
+    }
+    red[slice][threadIdx.x & 15] = v;
+    __syncthreads();
+    if (slice == 0 && col < cols) {
+        v = 0;
+#pragma unroll
+        for (int g = 0; g < 16; ++g) v += red[g][threadIdx.x];
+        out[col] = accumulate ? out[col] + v : v;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------
+// launches
+// ------------------------------------------------------------------------------------------------
+template <typename T, int LANES, int CH> static hipError_t forward_as(const NormForwardArgs<T>& a, hipStream_t s)
+{
+    const int64_t wgs = (a.rows + Group<LANES>::ROWS - 1) / Group<LANES>::ROWS;
+    if (wgs > 0x7FFFFFFF) return hipErrorInvalidValue;   // (refused by the entry point)
+    k_norm_forward<T, LANES, CH><<<dim3((unsigned)wgs), Group<LANES>::THREADS, 0, s>>>(a);
+    return hipGetLastError();
+}
+template <typename T> static hipError_t forward_of(const NormForwardLaunch& l, hipStream_t s)
+{
+    NormForwardArgs<T> a;
+    a.x = (const T*)l.x;
+    a.y = (T*)l.y;
+    a.ldx = l.ldx;
+    a.ldy = l.ldy;
+    a.rows = l.rows;
+    a.weight = l.weight;
+    a.bias = l.bias;
+    a.mean = l.mean;
+    a.rstd = l.rstd;
+    a.cols = (int32_t)l.cols;
+    a.param_f32 = l.param_dtype == FF_F32;
+    a.eps = l.eps;
+    a.inv_cols = 1.0f / (float)l.cols;
+    a.k = ckpt_ptr(l.q, l.e, l.cols);
+    a.r = {make_sr_key(l.seed, l.tag), l.round_mode == FF_ROUND_STOCHASTIC};
+    const int64_t chunks = (a.k.pitch / 8 + 3) / 4 * 4;   // (pad columns of the checkpoint included)
+    if (chunks <= 4) return forward_as<T, 4, 1>(a, s);
+    if (chunks <= 8) return forward_as<T, 8, 1>(a, s);
+    if (chunks <= 16) return forward_as<T, 16, 1>(a, s);
+    if (chunks <= 32) return forward_as<T, 32, 1>(a, s);
+    if (chunks <= 64) return forward_as<T, 64, 1>(a, s);
+    if (chunks <= 256) return forward_as<T, 256, 1>(a, s);
+    if (chunks <= 512) return forward_as<T, 256, 2>(a, s);
+    if (chunks <= 1024) return forward_as<T, 256, 4>(a, s);
+    if (chunks <= 2048) return forward_as<T, 512, 4>(a, s);
+    if (chunks <= 4096) return forward_as<T, 1024, 4>(a, s);
+    return forward_as<T, 1024, 0>(a, s);
+}
+hipError_t launch_norm_forward(const NormForwardLaunch& a, hipStream_t s)
+{
+    if (a.rows == 0) return hipSuccess;
+    return a.dtype == FF_F32 ? forward_of<float>(a, s) : a.dtype == FF_BF16 ? forward_of<bf16_t>(a, s) : forward_of<f16_t>(a, s);
+}
+
+// Lanes of a row and workgroups of the backward pass.
+struct NormPlan {
+    int lanes, ch;   // ch == 0: rows too wide for registers
+    int64_t wgs;     // workgroups that leave column sums
+};
+static NormPlan backward_plan(int64_t rows, int64_t cols)
+{
+    const int64_t chunks = (cols + 7) / 8;
+    NormPlan p;
+    if (chunks <= 64) {
+        p.ch = 1;
+        for (p.lanes = 4; p.lanes < chunks; p.lanes *= 2) {}
+    } else {
+        p.lanes = chunks <= 512 ? 256 : 512;
+        p.ch = chunks <= 256 ? 1 : chunks <= 1024 ? 2 : 0;
+    }
+    const int64_t per = p.lanes <= 64 ? 256 / p.lanes : 1;
+    const int64_t most = p.ch == 0 ? 64 : p.lanes <= 64 ? 1024 : 512;
+    const int64_t need = (rows + per - 1) / per;
+    p.wgs = need < most ? need : most;
+    return p;
+}
+static int64_t padded_cols(int64_t cols) { return (cols + 7) / 8 * 8; }
+size_t norm_backward_workspace(int64_t rows, int64_t cols)
+{
+    const NormPlan p = backward_plan(rows, cols);
+    size_t n = align_up((size_t)(p.wgs * 2 * padded_cols(cols)) * sizeof(float), 256);
+    if (p.ch == 0) n += align_up((size_t)rows * sizeof(float2), 256);
+    return n < FF_WS_MIN_BYTES ? FF_WS_MIN_BYTES : n;
+}
+
+template <typename T, bool KEPT> static hipError_t backward_of(const NormBackwardLaunch& l, hipStream_t s)
+{
+    const NormPlan p = backward_plan(l.rows, l.cols);
+    NormBackwardArgs<T> a;
+    a.dy = (const T*)l.dy;
+    a.x = (const T*)l.x;
+    a.dx = (T*)l.dx;
+    a.lddy = l.lddy;
+    a.ldx = l.ldx;
+    a.lddx = l.lddx;
+    a.rows = l.rows;
+    a.mean = l.mean;
+    a.rstd = l.rstd;
+    a.weight = l.weight;
+    a.cols = (int32_t)l.cols;
+    a.param_f32 = l.param_dtype == FF_F32;
+    a.sums = l.dweight || l.dbias;
+    a.inv_cols = 1.0f / (float)l.cols;
+    a.k = ckpt_ptr(l.q, l.e, l.cols);
+    a.part = (float*)l.ws;
+    a.pcols = padded_cols(l.cols);
+    a.row_sums = (float2*)((char*)l.ws + align_up((size_t)(p.wgs * 2 * a.pcols) * sizeof(float), 256));
+    const dim3 grid((unsigned)p.wgs);
+    if (l.rows > 0) {
+        if (p.ch == 0) {
+            if (a.dx) k_norm_row_sums<T, KEPT><<<dim3((unsigned)l.rows), 1024, 0, s>>>(a);
+            k_norm_backward_wide<T, KEPT><<<dim3((unsigned)((a.cols + 2047) / 2048), (unsigned)p.wgs), 256, 0, s>>>(a);
+        } else if (p.lanes == 4) {
+            k_norm_backward<T, KEPT, 4, 1><<<grid, 256, 0, s>>>(a);
+        } else if (p.lanes == 8) {
+            k_norm_backward<T, KEPT, 8, 1><<<grid, 256, 0, s>>>(a);
+        } else if (p.lanes == 16) {
+            k_norm_backward<T, KEPT, 16, 1><<<grid, 256, 0, s>>>(a);
+        } else if (p.lanes == 32) {
+            k_norm_backward<T, KEPT, 32, 1><<<grid, 256, 0, s>>>(a);
+        } else if (p.lanes == 64) {
+            k_norm_backward<T, KEPT, 64, 1><<<grid, 256, 0, s>>>(a);
+        } else if (p.ch == 1) {
+            k_norm_backward<T, KEPT, 256, 1><<<grid, 256, 0, s>>>(a);
+        } else if (p.lanes == 256) {
+            k_norm_backward<T, KEPT, 256, 2><<<grid, 256, 0, s>>>(a);
+        } else {
+            k_norm_backward<T, KEPT, 512, 2><<<grid, 512, 0, s>>>(a);
+        }
+        const hipError_t err = hipGetLastError();
+        if (err != hipSuccess) return err;
+    }
+    if (a.sums) {
+        k_norm_columns<<<dim3((unsigned)((a.cols + 15) / 16), 2), 256, 0, s>>>(a.part, (int)p.wgs, a.pcols, a.cols, l.dweight, l.dbias,
+                                                                                l.accumulate);
+        return hipGetLastError();
+    }
+    return hipSuccess;
+}
+hipError_t launch_norm_backward(const NormBackwardLaunch& a, hipStream_t s)
+{
+    if (a.dtype == FF_F32) return a.x ? backward_of<float, false>(a, s) : backward_of<float, true>(a, s);
+    if (a.dtype == FF_BF16) return a.x ? backward_of<bf16_t, false>(a, s) : backward_of<bf16_t, true>(a, s);
+    return a.x ? backward_of<f16_t, false>(a, s) : backward_of<f16_t, true>(a, s);
+}
+
+}  // namespace ffi
