@@ -156,6 +156,16 @@ template <typename T> __device__ __forceinline__ void store8(T* p, int n, const 
     store_raw(p, n, r);
 }
 
+// Values that the compiler is not to trace back.  It would keep what it made of them before instead of making it again, which takes more registers
+// than there are, or take them apart right behind the load, which waits for it there.
+__device__ __forceinline__ void opaque(u32x4& v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void opaque(u32x2& v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void opaque(Raw8<float>& r) { opaque(r.a); opaque(r.b); }
+__device__ __forceinline__ void opaque(Raw8<bf16_t>& r) { opaque(r.a); }
+__device__ __forceinline__ void opaque(Raw8<f16_t>& r) { opaque(r.a); }
+__device__ __forceinline__ void opaque(uint32_t& v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void opaque(float& v) { asm volatile("" : "+v"(v)); }
+
 // ---- a block's exponent byte and the codes of a chunk -------------------------------------------------------------------
 // A chunk is a lane's eight columns; the four lanes of a quad hold a block.
 __device__ __forceinline__ uint32_t quad_max_u32(uint32_t v)

@@ -155,10 +155,28 @@ __global__ __launch_bounds__(WG_T) __attribute__((amdgpu_waves_per_eu(BT == 256 
     const int8_t* const cq = a.c.q + ck;
     const uint8_t* const ce = a.c.e + cb;
     struct Chunk { Raw8<T> d; u32x2 q; uint32_t e; };
-    // A chunk of dy may reach into the next row (n not a multiple of eight); that stays inside the matrix but for the last row.
-    auto fetch = [&](int64_t step, int i) {
-        const int64_t m = step * S::BM + r0 + i * S::ROWS;
-        return Chunk{load_raw(dy + m * a.lddy, 8), *(const u32x2*)(cq + m * a.c.pitch), ce[m * a.c.epitch]};
+    // Steps in order, from scalar bases and this thread's fixed offsets.  A chunk of dy may reach into the next row (n not a multiple of
+    // eight); that stays inside the matrix but for the last row.
+    const uint32_t off_d = (uint32_t)(r0 * a.lddy + cn) * sizeof(T), off_q = (uint32_t)(r0 * a.c.pitch + ck), off_e = (uint32_t)(r0 * a.c.epitch) + cb;
+    const char* base_d = (const char*)a.dy + step0 * S::BM * a.lddy * sizeof(T);
+    const char* base_q = (const char*)a.c.q + step0 * S::BM * a.c.pitch;
+    const char* base_e = (const char*)a.c.e + step0 * S::BM * a.c.epitch;
+    auto fetch = [&](int i) {
+        const __amdgpu_buffer_rsrc_t bd = __builtin_amdgcn_make_buffer_rsrc((void*)base_d, 0, 0x7FFFFFFF, 0x00020000);
+        const __amdgpu_buffer_rsrc_t bq = __builtin_amdgcn_make_buffer_rsrc((void*)base_q, 0, 0x7FFFFFFF, 0x00020000);
+        const __amdgpu_buffer_rsrc_t be = __builtin_amdgcn_make_buffer_rsrc((void*)base_e, 0, 0x7FFFFFFF, 0x00020000);
+        const int at_d = (int)(i * S::ROWS * a.lddy * (int64_t)sizeof(T)), at_q = (int)(i * S::ROWS * a.c.pitch), at_e = (int)(i * S::ROWS * a.c.epitch);
+        Chunk c;
+        c.d.a = __builtin_amdgcn_raw_buffer_load_b128(bd, (int)off_d, at_d, 0);
+        if constexpr (sizeof(T) == 4) c.d.b = __builtin_amdgcn_raw_buffer_load_b128(bd, (int)off_d, at_d + 16, 0);
+        c.q = __builtin_amdgcn_raw_buffer_load_b64(bq, (int)off_q, at_q, 0);
+        c.e = __builtin_amdgcn_raw_buffer_load_b8(be, (int)off_e, at_e, 0);
+        return c;
+    };
+    auto advance = [&](bool more) {   // to the next step, or not beyond the last (which is then fetched again and used by nobody)
+        base_d += more ? S::BM * a.lddy * (int64_t)sizeof(T) : 0;
+        base_q += more ? S::BM * a.c.pitch : 0;
+        base_e += more ? S::BM * a.c.epitch : 0;
     };
     // Rows that do not exist are zero in both operands, columns beyond n too.
     auto fetch_last = [&](int64_t step, int i) {
@@ -167,7 +185,10 @@ __global__ __launch_bounds__(WG_T) __attribute__((amdgpu_waves_per_eu(BT == 256 
         if (m < a.rows) c = Chunk{load_raw(dy + m * a.lddy, min(8, a.n - cn)), *(const u32x2*)(cq + m * a.c.pitch), ce[m * a.c.epitch]};
         return c;
     };
-    auto put = [&](char* stage, int i, const Chunk& c) {
+    auto put = [&](char* stage, int i, Chunk c) {
+        opaque(c.d);
+        opaque(c.q);
+        opaque(c.e);
         const int m = r0 + i * S::ROWS;
         char* const at = stage + m * (BT * 2) + ((cc ^ swizzle<BT>(m)) << 4);
         u32x4 t[S::P];
@@ -217,27 +238,34 @@ __global__ __launch_bounds__(WG_T) __attribute__((amdgpu_waves_per_eu(BT == 256 
 
     const int64_t plain = min(step1, a.plain);   // steps read without looking at the end
     if (step0 < plain) {
-        Chunk c[S::CH];
+        constexpr int SETS = 2;   // steps on their way in registers
+        Chunk c[SETS][S::CH];
+        int64_t fetched = step0;  // the step that fetch() reads
+        auto fetch_step = [&](Chunk* to) {
+#pragma unroll
+            for (int i = 0; i < S::CH; ++i) to[i] = fetch(i);
+            advance(fetched + 1 < plain);
+            ++fetched;
+        };
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
+            fetch_step(c[0]);
 #pragma unroll
-            for (int i = 0; i < S::CH; ++i) c[i] = fetch(min(step0 + st, plain - 1), i);
-#pragma unroll
-            for (int i = 0; i < S::CH; ++i) put(lds + st * S::STAGE, i, c[i]);
+            for (int i = 0; i < S::CH; ++i) put(lds + st * S::STAGE, i, c[0][i]);
         }
 #pragma unroll
-        for (int i = 0; i < S::CH; ++i) c[i] = fetch(min(step0 + 2, plain - 1), i);
+        for (int st = 0; st < SETS; ++st) fetch_step(c[st]);
         meet();
         char *now = lds, *next = lds + S::STAGE, *after = lds + 2 * S::STAGE;
         v8bf fa = fragment_n(now, 0), fb[S::TI];
 #pragma unroll
         for (int j = 0; j < S::TI; ++j) fb[j] = fragment(now, at_k[j], 0);
-        for (int64_t step = step0; step < plain; ++step) {
-            const int64_t ahead = min(step + 3, plain - 1);   // (behind the last step: the last one again, which nobody uses)
+        auto work = [&](Chunk* set) {
             float sum[S::TI];
 #pragma unroll
             for (int i = 0; i < S::TI; ++i) sum[i] = 0;
             v8bf fb_next[S::TI];
+            constexpr int EVERY = S::PIECES / S::CH;   // pieces to a chunk
 #pragma unroll
             for (int piece = 0; piece < S::PIECES; ++piece) {
                 const int i = piece % S::TI, s = piece / (S::TI * S::P);
@@ -247,18 +275,31 @@ __global__ __launch_bounds__(WG_T) __attribute__((amdgpu_waves_per_eu(BT == 256 
 #pragma unroll
                 for (int j = 0; j < S::TI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
                 sum[i] = sum_of(fa, sum[i]);
-                constexpr int EVERY = S::PIECES / S::CH;
+                opaque(sum[i]);
                 if (piece % EVERY == 0) {
-                    put(after, piece / EVERY, c[piece / EVERY]);
-                    c[piece / EVERY] = fetch(ahead, piece / EVERY);
+                    put(after, piece / EVERY, set[piece / EVERY]);
+                    set[piece / EVERY] = fetch(piece / EVERY);
                 }
                 fa = fa_next;
                 if (last_of_sub && i == S::TI - 1) {
 #pragma unroll
                     for (int j = 0; j < S::TI; ++j) fb[j] = fb_next[j];
                 }
-                __builtin_amdgcn_sched_barrier(0);
+                if (piece % EVERY == EVERY - 1) {
+                    // One wavefront per SIMD: what is to run beside a matrix instruction has to stand behind it, before the next one.
+#pragma unroll
+                    for (int m = 0; m < EVERY * S::TI; ++m) {
+                        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // matrix
+                        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);   // LDS reads
+                        __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);   // vector arithmetic
+                        __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);   // LDS writes
+                        __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);   // loads
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
+            advance(fetched + 1 < plain);
+            ++fetched;
 #pragma unroll
             for (int i = 0; i < S::TI; ++i) db[i] += sum[i];
             meet();
@@ -266,6 +307,12 @@ __global__ __launch_bounds__(WG_T) __attribute__((amdgpu_waves_per_eu(BT == 256 
             now = next;
             next = after;
             after = first;
+        };
+        for (int64_t step = step0; step < plain; step += SETS) {
+            work(c[0]);
+#pragma unroll
+            for (int st = 1; st < SETS; ++st)
+                if (step + st < plain) work(c[st]);
         }
     }
     // what is left: the step with the last row, or all of them where a chunk may reach over several rows (n < 8)
@@ -411,7 +458,8 @@ template <typename T> static hipError_t wgrad_of(const CkptWgradLaunch& l, hipSt
     a.steps = p.steps;
     a.per = p.per;
     const int bm = plan_rows(Terms<T>::N, p.tile);
-    a.plain = l.n < 8 ? 0 : l.rows % bm == 0 && l.n % 8 == 0 ? p.steps : p.steps - 1;
+    const bool near = bm * l.lddy * (int64_t)sizeof(T) < int64_t(1) << 30;   // (offsets inside a step are 32 bits)
+    a.plain = l.n < 8 || !near ? 0 : l.rows % bm == 0 && l.n % 8 == 0 ? p.steps : p.steps - 1;
     a.gamma = l.gamma;
     a.beta = l.beta;
     a.param_kind = l.param_dtype;

@@ -184,14 +184,6 @@ template <typename T> struct NormBackwardArgs {
     float2* row_sums;   // rows too wide for registers: both means of every row
 };
 
-// Values that the compiler is not to trace back: it would keep what it made of them before instead of making it again, which takes more registers
-// than there are.
-__device__ __forceinline__ void opaque(u32x4& v) { asm volatile("" : "+v"(v)); }
-__device__ __forceinline__ void opaque(u32x2& v) { asm volatile("" : "+v"(v)); }
-__device__ __forceinline__ void opaque(Raw8<float>& r) { opaque(r.a); opaque(r.b); }
-__device__ __forceinline__ void opaque(Raw8<bf16_t>& r) { opaque(r.a); }
-__device__ __forceinline__ void opaque(Raw8<f16_t>& r) { opaque(r.a); }
-
 // Rows a group has in flight.
 template <typename T, int CH> constexpr int rows_ahead() { return (sizeof(T) == 4 ? 2 : 4) / CH; }
 
