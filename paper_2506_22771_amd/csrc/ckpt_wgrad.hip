@@ -9,7 +9,7 @@
 // (fp16) or three (fp32) bf16 terms, split by truncation, so that their sum is dy exactly (what lies below 2^-126 aside) and every product is exact: the only
 // roundings are those of the fp32 sums, as in a product of fp32 matrices, of which this is several times the rate.
 //
-// A workgroup of four wavefronts owns BT x BT outputs and walks over the rows in steps of BM.  Both operands lie in memory with the reduction (m)
+// A workgroup owns BT x BT outputs and walks over the rows in steps of BM.  Both operands lie in memory with the reduction (m)
 // as the slow axis.  A step's BM x BT elements go through registers, which is where codes become bf16 and dy its terms, into LDS as
 // they lie, and the fragments are read with the transposing LDS read.  Three stages of LDS: while a step is multiplied the one after the next is
 // written and the first fragments of the next are read already, so that no wavefront waits for LDS behind the barrier; registers hold the step after those.
@@ -24,8 +24,6 @@ typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
 typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
-
-constexpr int WG_T = 256;   // threads: two by two wavefronts
 
 template <typename T> struct Terms;
 template <> struct Terms<bf16_t> { static constexpr int N = 1; };
@@ -77,11 +75,8 @@ template <int BT> __device__ __forceinline__ int swizzle(int m)
 // times eight).  Infinities stay in the first term alone; a NaN is one in one of the terms.
 __device__ __forceinline__ void terms_of(const Raw8<bf16_t>& r, u32x4 t[1]) { t[0] = r.a; }
 __device__ __forceinline__ uint32_t high_pair(float lo, float hi) { return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u); }
-__device__ __forceinline__ float rest_of(float v)
-{
-    const float lead = __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);
-    return __builtin_fabsf(v) == __builtin_inff() ? 0.0f : v - lead;
-}
+__device__ __forceinline__ float lead_of(float v) { return __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); }
+__device__ __forceinline__ float rest_of(float v) { return __builtin_fabsf(v) == __builtin_inff() ? 0.0f : v - lead_of(v); }
 __device__ __forceinline__ void terms_of(const Raw8<f16_t>& r, u32x4 t[2])
 {
     float v[8];
@@ -101,7 +96,7 @@ __device__ __forceinline__ void terms_of(const Raw8<float>& r, u32x4 t[3])
         const float a = v[2 * i], b = v[2 * i + 1], a1 = rest_of(a), b1 = rest_of(b);
         t[0][i] = high_pair(a, b);
         t[1][i] = high_pair(a1, b1);
-        t[2][i] = high_pair(rest_of(a1), rest_of(b1));
+        t[2][i] = high_pair(a1 - lead_of(a1), b1 - lead_of(b1));   // (finite or NaN)
     }
 }
 
@@ -115,27 +110,32 @@ __device__ __forceinline__ float sum_of(v8bf f, float v)
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(f, f, 6, 7), one, v, false);
 }
 
-template <typename T, int BT> struct WgradTile {
+// Two by WK wavefronts.
+template <typename T, int BT, int WK> struct WgradTile {
     static constexpr int P = Terms<T>::N, BM = step_rows<T, BT>();
+    static constexpr int THREADS = 128 * WK;
     static constexpr int CPR = BT / 8;                   // chunks of a row
-    static constexpr int CH = BM * CPR / WG_T;           // chunks of a thread, of each operand
-    static constexpr int ROWS = WG_T / CPR;              // rows between a thread's chunks
+    static constexpr int CH = BM * CPR / THREADS;        // chunks of a thread, of each operand
+    static constexpr int ROWS = THREADS / CPR;           // rows between a thread's chunks
     static constexpr int PLANE = BM * BT * 2;            // bytes of one term
     static constexpr int STAGE = (P + 1) * PLANE;
     static constexpr int SUB = BM / 16;                  // matrix instructions along a step
-    static constexpr int WT = BT / 2, TI = WT / 32;      // a wavefront's outputs, in tiles of 32
-    static constexpr int PIECES = SUB * P * TI;          // a wavefront's fragments of dy in a step, TI matrix instructions each
+    static constexpr int TI = BT / 64, TJ = BT / (32 * WK);   // a wavefront's outputs, in tiles of 32
+    static constexpr int PIECES = SUB * P * TI;          // a wavefront's fragments of dy in a step, TJ matrix instructions each
+    static constexpr int EVERY = PIECES / CH;            // pieces to a chunk
+    // Steps on their way in registers: as many as a step's matrix instructions (32 clocks each) need to cover some 2500 clocks.
+    static constexpr int SETS = BT == 256 ? 2 : BT == 128 ? 4 : 6;
     static constexpr int LDS = 3 * STAGE;
-    static_assert(CH >= 1 && LDS <= 160 * 1024 && ROWS % 8 == 0 && PIECES % CH == 0, "tile");
+    static_assert(CH >= 1 && LDS <= 160 * 1024 && ROWS % 8 == 0 && PIECES % CH == 0 && TJ <= TI, "tile");
 };
 
-template <typename T, int BT>
-__global__ __launch_bounds__(WG_T) __attribute__((amdgpu_waves_per_eu(BT == 256 ? 1 : 2))) void k_ckpt_wgrad(WgradArgs a)
+template <typename T, int BT, int WK>
+__global__ __launch_bounds__(128 * WK) __attribute__((amdgpu_waves_per_eu(BT == 256 ? WK / 2 : 2))) void k_ckpt_wgrad(WgradArgs a)
 {
-    using S = WgradTile<T, BT>;
+    using S = WgradTile<T, BT, WK>;
     __shared__ __attribute__((aligned(16))) char lds[S::LDS];
     const int tid = threadIdx.x, lane = tid & 63, lr = lane & 31, lh = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wn = wave >> 1, wk = wave & 1;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wn = wave / WK, wk = wave % WK;
     // Workgroups go to the eight XCDs in turn: each takes consecutive tiles, in bands of four tiles of n, so that its L2 holds few panels.
     const int items = a.tiles_n * a.tiles_k * a.splits, per_xcd = (items + 7) >> 3;
     const int item = (int)(blockIdx.x & 7) * per_xcd + (int)(blockIdx.x >> 3);
@@ -203,25 +203,24 @@ __global__ __launch_bounds__(WG_T) __attribute__((amdgpu_waves_per_eu(BT == 256 
         *(u32x4*)(at + S::P * S::PLANE) = x;
     };
 
-    v16f acc[S::TI][S::TI];
+    v16f acc[S::TI][S::TJ];
     float db[S::TI];
 #pragma unroll
     for (int i = 0; i < S::TI; ++i) {
         db[i] = 0;
 #pragma unroll
-        for (int j = 0; j < S::TI; ++j)
+        for (int j = 0; j < S::TJ; ++j)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][j][v] = 0;
     }
     // A lane's place in a transposing read: row 8 lh + (lane & 15) / 4 of a 16-row piece (and four rows on for the second half of a fragment, where
     // the swizzle is the same), columns 16 ((lane >> 4) & 1) + 4 (lane & 3) of a 32-column tile.
     const int tr_row = 8 * lh + ((lane & 15) >> 2), tr_at = tr_row * (BT * 2) + ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) << 4) + 8 * (lane & 1);
-    int at_n[S::TI], at_k[S::TI];
+    int at_n[S::TI], at_k[S::TJ];
 #pragma unroll
-    for (int i = 0; i < S::TI; ++i) {
-        at_n[i] = tr_at + ((((wn * S::WT + 32 * i) >> 3) ^ swizzle<BT>(tr_row)) << 4);
-        at_k[i] = tr_at + ((((wk * S::WT + 32 * i) >> 3) ^ swizzle<BT>(tr_row)) << 4) + S::P * S::PLANE;
-    }
+    for (int i = 0; i < S::TI; ++i) at_n[i] = tr_at + ((((wn * S::TI + i) << 2) ^ swizzle<BT>(tr_row)) << 4);
+#pragma unroll
+    for (int j = 0; j < S::TJ; ++j) at_k[j] = tr_at + ((((wk * S::TJ + j) << 2) ^ swizzle<BT>(tr_row)) << 4) + S::P * S::PLANE;
     auto fragment = [&](const char* stage, int at, int more) {   // more: a constant
         const v4s lo = tr_read16(stage + at + more), hi = tr_read16(stage + at + more + 4 * BT * 2);
         return __builtin_bit_cast(v8bf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -238,7 +237,7 @@ __global__ __launch_bounds__(WG_T) __attribute__((amdgpu_waves_per_eu(BT == 256 
 
     const int64_t plain = min(step1, a.plain);   // steps read without looking at the end
     if (step0 < plain) {
-        constexpr int SETS = 2;   // steps on their way in registers
+        constexpr int SETS = S::SETS;
         Chunk c[SETS][S::CH];
         int64_t fetched = step0;  // the step that fetch() reads
         auto fetch_step = [&](Chunk* to) {
@@ -257,23 +256,23 @@ __global__ __launch_bounds__(WG_T) __attribute__((amdgpu_waves_per_eu(BT == 256 
         for (int st = 0; st < SETS; ++st) fetch_step(c[st]);
         meet();
         char *now = lds, *next = lds + S::STAGE, *after = lds + 2 * S::STAGE;
-        v8bf fa = fragment_n(now, 0), fb[S::TI];
+        v8bf fa = fragment_n(now, 0), fb[S::TJ];
 #pragma unroll
-        for (int j = 0; j < S::TI; ++j) fb[j] = fragment(now, at_k[j], 0);
+        for (int j = 0; j < S::TJ; ++j) fb[j] = fragment(now, at_k[j], 0);
         auto work = [&](Chunk* set) {
             float sum[S::TI];
 #pragma unroll
             for (int i = 0; i < S::TI; ++i) sum[i] = 0;
-            v8bf fb_next[S::TI];
-            constexpr int EVERY = S::PIECES / S::CH;   // pieces to a chunk
+            v8bf fb_next[S::TJ];
+            constexpr int EVERY = S::EVERY;
 #pragma unroll
             for (int piece = 0; piece < S::PIECES; ++piece) {
                 const int i = piece % S::TI, s = piece / (S::TI * S::P);
                 const bool last_of_sub = (piece + S::TI) / (S::TI * S::P) > s;   // the last term's pieces: the next fragments of k are read
                 const v8bf fa_next = piece + 1 < S::PIECES ? fragment_n(now, piece + 1) : fragment_n(next, 0);
-                if (last_of_sub) fb_next[i] = s + 1 < S::SUB ? fragment(now, at_k[i], (s + 1) * 16 * BT * 2) : fragment(next, at_k[i], 0);
+                if (last_of_sub && i < S::TJ) fb_next[i] = s + 1 < S::SUB ? fragment(now, at_k[i], (s + 1) * 16 * BT * 2) : fragment(next, at_k[i], 0);
 #pragma unroll
-                for (int j = 0; j < S::TI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
+                for (int j = 0; j < S::TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
                 sum[i] = sum_of(fa, sum[i]);
                 opaque(sum[i]);
                 if (piece % EVERY == 0) {
@@ -283,12 +282,12 @@ __global__ __launch_bounds__(WG_T) __attribute__((amdgpu_waves_per_eu(BT == 256 
                 fa = fa_next;
                 if (last_of_sub && i == S::TI - 1) {
 #pragma unroll
-                    for (int j = 0; j < S::TI; ++j) fb[j] = fb_next[j];
+                    for (int j = 0; j < S::TJ; ++j) fb[j] = fb_next[j];
                 }
                 if (piece % EVERY == EVERY - 1) {
                     // One wavefront per SIMD: what is to run beside a matrix instruction has to stand behind it, before the next one.
 #pragma unroll
-                    for (int m = 0; m < EVERY * S::TI; ++m) {
+                    for (int m = 0; m < EVERY * S::TJ; ++m) {
                         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // matrix
                         __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);   // LDS reads
                         __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);   // vector arithmetic
@@ -308,12 +307,15 @@ __global__ __launch_bounds__(WG_T) __attribute__((amdgpu_waves_per_eu(BT == 256 
             next = after;
             after = first;
         };
-        for (int64_t step = step0; step < plain; step += SETS) {
-            work(c[0]);
+        // (Whole rounds without a branch in them: where a step may be left out the compiler counts on the fewest loads under way and
+        // waits for nearly all of them.)
+        int64_t step = step0;
+        for (; step + SETS <= plain; step += SETS)
 #pragma unroll
-            for (int st = 1; st < SETS; ++st)
-                if (step + st < plain) work(c[st]);
-        }
+            for (int st = 0; st < SETS; ++st) work(c[st]);
+#pragma unroll
+        for (int st = 0; st < SETS - 1; ++st)
+            if (step + st < plain) work(c[st]);
     }
     // what is left: the step with the last row, or all of them where a chunk may reach over several rows (n < 8)
     for (int64_t step = max(step0, plain); step < step1; ++step) {
@@ -323,15 +325,15 @@ __global__ __launch_bounds__(WG_T) __attribute__((amdgpu_waves_per_eu(BT == 256 
         meet();
 #pragma nounroll
         for (int s = 0; s < S::SUB; ++s) {
-            v8bf fb[S::TI];
+            v8bf fb[S::TJ];
 #pragma unroll
-            for (int j = 0; j < S::TI; ++j) fb[j] = fragment(lds + s * 16 * BT * 2, at_k[j], 0);
+            for (int j = 0; j < S::TJ; ++j) fb[j] = fragment(lds + s * 16 * BT * 2, at_k[j], 0);
 #pragma unroll
             for (int piece = 0; piece < S::P * S::TI; ++piece) {
                 const int i = piece % S::TI;
                 const v8bf fa = fragment_n(lds + s * 16 * BT * 2, piece);
 #pragma unroll
-                for (int j = 0; j < S::TI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
+                for (int j = 0; j < S::TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
                 db[i] = sum_of(fa, db[i]);
             }
         }
@@ -343,27 +345,27 @@ __global__ __launch_bounds__(WG_T) __attribute__((amdgpu_waves_per_eu(BT == 256 
 #pragma unroll
     for (int i = 0; i < S::TI; ++i) {
         const float both = db[i] + __shfl_xor(db[i], 32);
-        if (lh == 0 && wk == 0) sums[wn * S::WT + 32 * i + lr] = both;
+        if (lh == 0 && wk == 0) sums[32 * (wn * S::TI + i) + lr] = both;
     }
     __syncthreads();
     const bool whole = a.splits == 1;
     float* const out = whole ? a.dw : a.part + (int64_t)split * a.n * a.k;
     if (tk == 0)
-        for (int i = tid; i < BT && n0 + i < a.n; i += WG_T) {
+        for (int i = tid; i < BT && n0 + i < a.n; i += S::THREADS) {
             const float v = sums[i];
             if (!whole) a.part[(int64_t)a.splits * a.n * a.k + (int64_t)split * a.n + n0 + i] = v;
             else if (a.db) a.db[n0 + i] = a.accumulate ? a.db[n0 + i] + v : v;
         }
 #pragma unroll
-    for (int j = 0; j < S::TI; ++j) {
-        const int k = k0 + wk * S::WT + 32 * j + lr;
+    for (int j = 0; j < S::TJ; ++j) {
+        const int k = k0 + 32 * (wk * S::TJ + j) + lr;
         if (k >= a.k) continue;
         const float g = whole ? param_at(a.gamma, a.param_kind, k, 1.0f) : 1.0f, b = whole ? param_at(a.beta, a.param_kind, k, 0.0f) : 0.0f;
 #pragma unroll
         for (int i = 0; i < S::TI; ++i)
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
-                const int nl = wn * S::WT + 32 * i + (v & 3) + 8 * (v >> 2) + 4 * lh, n = n0 + nl;
+                const int nl = 32 * (wn * S::TI + i) + (v & 3) + 8 * (v >> 2) + 4 * lh, n = n0 + nl;
                 if (n >= a.n) continue;
                 float r = acc[i][j][v];
                 float* const to = out + (int64_t)n * a.k + k;
@@ -469,9 +471,9 @@ template <typename T> static hipError_t wgrad_of(const CkptWgradLaunch& l, hipSt
     a.part = (float*)l.ws;
     if (l.rows > 0) {
         const unsigned grid = (unsigned)(((int64_t)a.tiles_n * a.tiles_k * a.splits + 7) / 8 * 8);
-        if (p.tile == 256) k_ckpt_wgrad<T, 256><<<grid, WG_T, 0, s>>>(a);
-        else if (p.tile == 128) k_ckpt_wgrad<T, 128><<<grid, WG_T, 0, s>>>(a);
-        else k_ckpt_wgrad<T, 64><<<grid, WG_T, 0, s>>>(a);
+        if (p.tile == 256) k_ckpt_wgrad<T, 256, 4><<<grid, 512, 0, s>>>(a);
+        else if (p.tile == 128) k_ckpt_wgrad<T, 128, 2><<<grid, 256, 0, s>>>(a);
+        else k_ckpt_wgrad<T, 64, 2><<<grid, 256, 0, s>>>(a);
         const hipError_t err = hipGetLastError();
         if (err != hipSuccess) return err;
     }
