@@ -46,7 +46,8 @@ struct WgradArgs {
     float* dw;
     float* db;
     int32_t accumulate;
-    float* part;             // splits > 1: [splits][n][k], then [splits][n]
+    float* part;             // splits > 1: a split's dw and db, `stride` apart
+    int64_t stride;
 };
 
 __device__ __forceinline__ float param_at(const void* p, int kind, int64_t at, float none)
@@ -110,6 +111,15 @@ __device__ __forceinline__ float sum_of(v8bf f, float v)
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(f, f, 6, 7), one, v, false);
 }
 
+// f(0), ..., f(N - 1), as constants
+template <int I, int N, typename F> __device__ __forceinline__ void each_of(F&& f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        each_of<I + 1, N>(f);
+    }
+}
+
 // Two by WK wavefronts.
 template <typename T, int BT, int WK> struct WgradTile {
     static constexpr int P = Terms<T>::N, BM = step_rows<T, BT>();
@@ -120,11 +130,14 @@ template <typename T, int BT, int WK> struct WgradTile {
     static constexpr int PLANE = BM * BT * 2;            // bytes of one term
     static constexpr int STAGE = (P + 1) * PLANE;
     static constexpr int SUB = BM / 16;                  // matrix instructions along a step
+    static_assert(WK >= BT / 64 || BT / 64 == 1, "sums of dy");
     static constexpr int TI = BT / 64, TJ = BT / (32 * WK);   // a wavefront's outputs, in tiles of 32
     static constexpr int PIECES = SUB * P * TI;          // a wavefront's fragments of dy in a step, TJ matrix instructions each
     static constexpr int EVERY = PIECES / CH;            // pieces to a chunk
     // Steps on their way in registers: as many as a step's matrix instructions (32 clocks each) need to cover some 2500 clocks.
     static constexpr int SETS = BT == 256 ? 2 : BT == 128 ? 4 : 6;
+    // Fragments of dy read ahead: a read takes some 130 clocks and more, a piece 32 TJ of its SIMD's matrix pipe.
+    static constexpr int AHEAD = PIECES < 3 ? 2 : BT == 256 ? 2 : 3;
     static constexpr int LDS = 3 * STAGE;
     static_assert(CH >= 1 && LDS <= 160 * 1024 && ROWS % 8 == 0 && PIECES % CH == 0 && TJ <= TI, "tile");
 };
@@ -204,21 +217,20 @@ __global__ __launch_bounds__(128 * WK) __attribute__((amdgpu_waves_per_eu(BT == 
     };
 
     v16f acc[S::TI][S::TJ];
-    float db[S::TI];
+    float db = 0;   // this lane's share of the sums of dy, for the tile wk % TI of its wavefront's rows n
 #pragma unroll
-    for (int i = 0; i < S::TI; ++i) {
-        db[i] = 0;
+    for (int i = 0; i < S::TI; ++i)
 #pragma unroll
         for (int j = 0; j < S::TJ; ++j)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][j][v] = 0;
-    }
     // A lane's place in a transposing read: row 8 lh + (lane & 15) / 4 of a 16-row piece (and four rows on for the second half of a fragment, where
     // the swizzle is the same), columns 16 ((lane >> 4) & 1) + 4 (lane & 3) of a 32-column tile.
     const int tr_row = 8 * lh + ((lane & 15) >> 2), tr_at = tr_row * (BT * 2) + ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) << 4) + 8 * (lane & 1);
     int at_n[S::TI], at_k[S::TJ];
 #pragma unroll
     for (int i = 0; i < S::TI; ++i) at_n[i] = tr_at + ((((wn * S::TI + i) << 2) ^ swizzle<BT>(tr_row)) << 4);
+    const int at_sum = tr_at + ((((wn * S::TI + wk % S::TI) << 2) ^ swizzle<BT>(tr_row)) << 4);
 #pragma unroll
     for (int j = 0; j < S::TJ; ++j) at_k[j] = tr_at + ((((wk * S::TJ + j) << 2) ^ swizzle<BT>(tr_row)) << 4) + S::P * S::PLANE;
     auto fragment = [&](const char* stage, int at, int more) {   // more: a constant
@@ -256,38 +268,47 @@ __global__ __launch_bounds__(128 * WK) __attribute__((amdgpu_waves_per_eu(BT == 
         for (int st = 0; st < SETS; ++st) fetch_step(c[st]);
         meet();
         char *now = lds, *next = lds + S::STAGE, *after = lds + 2 * S::STAGE;
-        v8bf fa = fragment_n(now, 0), fb[S::TJ];
+        v8bf fa[S::AHEAD], fb[S::TJ];
+#pragma unroll
+        for (int i = 0; i < S::AHEAD; ++i) fa[i] = fragment_n(now, i);
 #pragma unroll
         for (int j = 0; j < S::TJ; ++j) fb[j] = fragment(now, at_k[j], 0);
-        auto work = [&](Chunk* set) {
-            float sum[S::TI];
-#pragma unroll
-            for (int i = 0; i < S::TI; ++i) sum[i] = 0;
-            v8bf fb_next[S::TJ];
-            constexpr int EVERY = S::EVERY;
+        v8bf fb_next[S::TJ];
+        v8bf fs;
+        auto work = [&](auto set) {
+            constexpr int ST = decltype(set)::value;
 #pragma unroll
             for (int piece = 0; piece < S::PIECES; ++piece) {
-                const int i = piece % S::TI, s = piece / (S::TI * S::P);
-                const bool last_of_sub = (piece + S::TI) / (S::TI * S::P) > s;   // the last term's pieces: the next fragments of k are read
-                const v8bf fa_next = piece + 1 < S::PIECES ? fragment_n(now, piece + 1) : fragment_n(next, 0);
-                if (last_of_sub && i < S::TJ) fb_next[i] = s + 1 < S::SUB ? fragment(now, at_k[i], (s + 1) * 16 * BT * 2) : fragment(next, at_k[i], 0);
+                const int i = piece % S::TI, p = piece / S::TI % S::P, s = piece / (S::TI * S::P), chunk = piece / S::EVERY;
+                if (piece % (S::TI * S::P) == 0) {   // the next sixteen rows' fragments of k
 #pragma unroll
-                for (int j = 0; j < S::TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
-                sum[i] = sum_of(fa, sum[i]);
-                opaque(sum[i]);
-                if (piece % EVERY == 0) {
-                    put(after, piece / EVERY, set[piece / EVERY]);
-                    set[piece / EVERY] = fetch(piece / EVERY);
+                    for (int j = 0; j < S::TJ; ++j)
+                        fb_next[j] = s + 1 < S::SUB ? fragment(now, at_k[j], (s + 1) * 16 * BT * 2) : fragment(next, at_k[j], 0);
                 }
-                fa = fa_next;
-                if (last_of_sub && i == S::TI - 1) {
+                const v8bf f = fa[0];
+#pragma unroll
+                for (int d = 0; d + 1 < S::AHEAD; ++d) fa[d] = fa[d + 1];
+                constexpr int AT = S::PIECES - S::AHEAD;
+                fa[S::AHEAD - 1] = piece < AT ? fragment_n(now, piece + S::AHEAD) : fragment_n(next, piece - AT);
+                if (S::TI > 1 && i == 0) fs = fragment(now, at_sum, s * 16 * BT * 2 + p * S::PLANE);
+#pragma unroll
+                for (int j = 0; j < S::TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, fb[j], acc[i][j], 0, 0, 0);
+                if (i == S::TI - 1) {
+                    db += sum_of(S::TI > 1 ? fs : f, 0.0f);
+                    opaque(db);
+                }
+                if (piece % S::EVERY == 0) {
+                    put(after, chunk, c[ST][chunk]);
+                    c[ST][chunk] = fetch(chunk);
+                }
+                if ((piece + 1) % (S::TI * S::P) == 0) {
 #pragma unroll
                     for (int j = 0; j < S::TJ; ++j) fb[j] = fb_next[j];
                 }
-                if (piece % EVERY == EVERY - 1) {
-                    // One wavefront per SIMD: what is to run beside a matrix instruction has to stand behind it, before the next one.
+                if (piece % S::EVERY == S::EVERY - 1) {
+                    // What is to run beside a matrix instruction has to stand behind it, before the next one.
 #pragma unroll
-                    for (int m = 0; m < EVERY * S::TJ; ++m) {
+                    for (int m = 0; m < S::EVERY * S::TJ; ++m) {
                         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // matrix
                         __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);   // LDS reads
                         __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);   // vector arithmetic
@@ -299,8 +320,6 @@ __global__ __launch_bounds__(128 * WK) __attribute__((amdgpu_waves_per_eu(BT == 
             }
             advance(fetched + 1 < plain);
             ++fetched;
-#pragma unroll
-            for (int i = 0; i < S::TI; ++i) db[i] += sum[i];
             meet();
             char* const first = now;
             now = next;
@@ -310,12 +329,10 @@ __global__ __launch_bounds__(128 * WK) __attribute__((amdgpu_waves_per_eu(BT == 
         // (Whole rounds without a branch in them: where a step may be left out the compiler counts on the fewest loads under way and
         // waits for nearly all of them.)
         int64_t step = step0;
-        for (; step + SETS <= plain; step += SETS)
-#pragma unroll
-            for (int st = 0; st < SETS; ++st) work(c[st]);
-#pragma unroll
-        for (int st = 0; st < SETS - 1; ++st)
-            if (step + st < plain) work(c[st]);
+        for (; step + SETS <= plain; step += SETS) each_of<0, SETS>(work);
+        each_of<0, SETS - 1>([&](auto st) {
+            if (step + decltype(st)::value < plain) work(st);
+        });
     }
     // what is left: the step with the last row, or all of them where a chunk may reach over several rows (n < 8)
     for (int64_t step = max(step0, plain); step < step1; ++step) {
@@ -334,70 +351,69 @@ __global__ __launch_bounds__(128 * WK) __attribute__((amdgpu_waves_per_eu(BT == 
                 const v8bf fa = fragment_n(lds + s * 16 * BT * 2, piece);
 #pragma unroll
                 for (int j = 0; j < S::TJ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
-                db[i] = sum_of(fa, db[i]);
+                if (i == wk % S::TI) db += sum_of(fa, 0.0f);
             }
         }
     }
     meet();
 
-    // sums of dy, which both wavefronts of a half of n have: the halves of a wavefront, through LDS (which nothing reads any more)
+    // sums of dy, in LDS (which nothing reads any more): both halves of a wavefront have eight of sixteen rows
     float* const sums = (float*)lds;
-#pragma unroll
-    for (int i = 0; i < S::TI; ++i) {
-        const float both = db[i] + __shfl_xor(db[i], 32);
-        if (lh == 0 && wk == 0) sums[32 * (wn * S::TI + i) + lr] = both;
-    }
+    db += __shfl_xor(db, 32);
+    if (lh == 0 && wk < S::TI) sums[32 * (wn * S::TI + wk) + lr] = db;
     __syncthreads();
-    const bool whole = a.splits == 1;
-    float* const out = whole ? a.dw : a.part + (int64_t)split * a.n * a.k;
-    if (tk == 0)
-        for (int i = tid; i < BT && n0 + i < a.n; i += S::THREADS) {
-            const float v = sums[i];
-            if (!whole) a.part[(int64_t)a.splits * a.n * a.k + (int64_t)split * a.n + n0 + i] = v;
-            else if (a.db) a.db[n0 + i] = a.accumulate ? a.db[n0 + i] + v : v;
-        }
+    const bool whole = a.splits == 1, add = whole && a.accumulate;
+    float* const out = whole ? a.dw : a.part + (int64_t)split * a.stride;
+    float* const out_db = whole ? a.db : a.part + (int64_t)split * a.stride + (int64_t)a.n * a.k;
+    if (tk == 0 && out_db && tid < BT && n0 + tid < a.n) out_db[n0 + tid] = add ? out_db[n0 + tid] + sums[tid] : sums[tid];
+    // Both parts of the result are linear in the rows: gamma and beta are applied to every split's sums.
 #pragma unroll
     for (int j = 0; j < S::TJ; ++j) {
         const int k = k0 + 32 * (wk * S::TJ + j) + lr;
         if (k >= a.k) continue;
-        const float g = whole ? param_at(a.gamma, a.param_kind, k, 1.0f) : 1.0f, b = whole ? param_at(a.beta, a.param_kind, k, 0.0f) : 0.0f;
+        const float g = param_at(a.gamma, a.param_kind, k, 1.0f), b = param_at(a.beta, a.param_kind, k, 0.0f);
 #pragma unroll
         for (int i = 0; i < S::TI; ++i)
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 const int nl = 32 * (wn * S::TI + i) + (v & 3) + 8 * (v >> 2) + 4 * lh, n = n0 + nl;
                 if (n >= a.n) continue;
-                float r = acc[i][j][v];
+                float r = g * acc[i][j][v];
+                if (a.beta) r = __builtin_fmaf(b, sums[nl], r);
                 float* const to = out + (int64_t)n * a.k + k;
-                if (whole) {
-                    r = g * r;
-                    if (a.beta) r = __builtin_fmaf(b, sums[nl], r);
-                    if (a.accumulate) r += *to;
-                }
-                *to = r;
+                *to = add ? *to + r : r;
             }
     }
 }
 
-// Adds the splits' partial sums, in order, and applies gamma and beta.  No splits (no rows): zero.
+// Adds the splits' results in order, four values a thread: dw, then db.  No splits (no rows): zero.
 __global__ __launch_bounds__(256) void k_ckpt_wgrad_sum(WgradArgs a)
 {
-    const float* const pdb = a.part + (int64_t)a.splits * a.n * a.k;
-    const int64_t size = (int64_t)a.n * a.k;
-    const int n = blockIdx.y;
-    float d = 0;
-    if (a.beta || a.db)
-        for (int s = 0; s < a.splits; ++s) d += pdb[(int64_t)s * a.n + n];
-    if (a.db && blockIdx.x == 0 && threadIdx.x == 0) a.db[n] = a.accumulate ? a.db[n] + d : d;
-    const int k = (int)(blockIdx.x * 256 + threadIdx.x);
-    if (k >= a.k) return;
-    const int64_t at = (int64_t)n * a.k + k;
-    float v = 0;
-#pragma unroll 8
-    for (int s = 0; s < a.splits; ++s) v += a.part[s * size + at];
-    v = param_at(a.gamma, a.param_kind, k, 1.0f) * v;
-    if (a.beta) v = __builtin_fmaf(param_at(a.beta, a.param_kind, k, 0.0f), d, v);
-    a.dw[at] = a.accumulate ? a.dw[at] + v : v;
+    const int64_t size = (int64_t)a.n * a.k, at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, end = size + (a.db ? a.n : 0);
+    if (at >= end) return;
+    float4 v = make_float4(0, 0, 0, 0);
+    const float* p = a.part + at;   // (a split's results are followed by room up to `stride`, a multiple of four)
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s, p += a.stride) {
+        const float4 t = *(const float4*)p;
+        v = make_float4(v.x + t.x, v.y + t.y, v.z + t.z, v.w + t.w);
+    }
+    const float r[4] = {v.x, v.y, v.z, v.w};
+    if (at + 4 <= size) {
+        float* const to = a.dw + at;
+        u32x4 o;
+        if (a.accumulate) o = read_as<u32x4>(to);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = __float_as_uint(a.accumulate ? __uint_as_float(o[i]) + r[i] : r[i]);
+        write_as<u32x4>(to, o);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (at + i < end) {
+                float* const to = at + i < size ? a.dw + at + i : a.db + (at + i - size);
+                *to = a.accumulate ? *to + r[i] : r[i];
+            }
+    }
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -433,12 +449,13 @@ static WgradPlan wgrad_plan(int64_t rows, int64_t n, int64_t k, int terms)
     }
     return best;
 }
+static int64_t part_stride(int64_t n, int64_t k) { return (n * k + n + 3) & ~int64_t(3); }
 size_t ckpt_wgrad_workspace(int64_t rows, int64_t n, int64_t k)
 {
     size_t most = FF_WS_MIN_BYTES;
     for (int terms = 1; terms <= 3; ++terms) {
         const WgradPlan p = wgrad_plan(rows, n, k, terms);
-        const size_t need = p.splits > 1 ? align_up((size_t)p.splits * (size_t)(n * k + n) * sizeof(float), 256) : 0;
+        const size_t need = p.splits > 1 ? align_up((size_t)p.splits * (size_t)part_stride(n, k) * sizeof(float), 256) : 0;
         if (need > most) most = need;
     }
     return most;
@@ -469,6 +486,7 @@ template <typename T> static hipError_t wgrad_of(const CkptWgradLaunch& l, hipSt
     a.db = l.db;
     a.accumulate = l.accumulate;
     a.part = (float*)l.ws;
+    a.stride = part_stride(l.n, l.k);
     if (l.rows > 0) {
         const unsigned grid = (unsigned)(((int64_t)a.tiles_n * a.tiles_k * a.splits + 7) / 8 * 8);
         if (p.tile == 256) k_ckpt_wgrad<T, 256, 4><<<grid, 512, 0, s>>>(a);
@@ -478,7 +496,8 @@ template <typename T> static hipError_t wgrad_of(const CkptWgradLaunch& l, hipSt
         if (err != hipSuccess) return err;
     }
     if (a.splits != 1) {
-        k_ckpt_wgrad_sum<<<dim3((unsigned)((a.k + 255) / 256), (unsigned)a.n), 256, 0, s>>>(a);
+        const int64_t all = (int64_t)a.n * a.k + a.n;
+        k_ckpt_wgrad_sum<<<dim3((unsigned)((all + 1023) / 1024)), 256, 0, s>>>(a);
         return hipGetLastError();
     }
     return hipSuccess;
