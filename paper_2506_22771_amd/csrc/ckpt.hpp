@@ -164,6 +164,7 @@ __device__ __forceinline__ void opaque(Raw8<float>& r) { opaque(r.a); opaque(r.b
 __device__ __forceinline__ void opaque(Raw8<bf16_t>& r) { opaque(r.a); }
 __device__ __forceinline__ void opaque(Raw8<f16_t>& r) { opaque(r.a); }
 __device__ __forceinline__ void opaque(uint32_t& v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void opaque_uniform(int& v) { asm volatile("" : "+s"(v)); }
 __device__ __forceinline__ void opaque(float& v) { asm volatile("" : "+v"(v)); }
 
 // ---- a block's exponent byte and the codes of a chunk -------------------------------------------------------------------

@@ -64,6 +64,25 @@ template <typename T> __device__ __forceinline__ void load_param(const void* p, 
     }
 }
 
+// A row's chunk c, n of whose columns exist.  RAGGED: rows end inside a chunk.  Where they do not, a chunk is there or is not, and what is not is
+// read from the row's first chunk and made zero: no branch, behind which the compiler would count on fewer loads under way than there are.
+template <bool RAGGED, typename T> __device__ __forceinline__ Raw8<T> row_chunk(const T* row, int c, int n)
+{
+    if constexpr (RAGGED) return load_raw(row + 8 * c, n);
+    Raw8<T> r = load_raw(row + (n > 0 ? 8 * c : 0), 8);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r.a[i] = n > 0 ? r.a[i] : 0u;
+        if constexpr (sizeof(T) == 4) r.b[i] = n > 0 ? r.b[i] : 0u;
+    }
+    return r;
+}
+template <bool RAGGED, typename T> __device__ __forceinline__ void row_store(T* row, int c, int n, const float v[8])
+{
+    if constexpr (RAGGED) store8(row + 8 * c, n, v);
+    else if (n > 0) store8(row + 8 * c, 8, v);
+}
+
 template <typename T> struct NormForwardArgs {
     const T* x;
     T* y;
@@ -78,88 +97,143 @@ template <typename T> struct NormForwardArgs {
     CkptRound r;
 };
 
-// CH chunks of a lane; CH == 0: any number, read three times (rows beyond 32768 columns, which the caches hold).
-template <typename T, int LANES, int CH>
+// CH chunks of a lane.  Workgroups of several wavefronts to a row take row after row, with the parameters in registers and the next row's values on
+// their way; the others take one row per group, whose few parameters the cache holds.
+template <typename T, int LANES, int CH, bool RAGGED>
 __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForwardArgs<T> a)
 {
     constexpr int W = LANES > 64 ? LANES / 64 : 1;
-    __shared__ float red[2][W];
+    constexpr bool MANY = LANES > 64 && LANES < 1024;   // (1024 lanes have no registers to spare)
+    __shared__ float red[2][W];   // (a sum's words are written again behind the other sum's barrier)
     const int j = threadIdx.x % LANES;
-    const int64_t row_at = (int64_t)blockIdx.x * Group<LANES>::ROWS + threadIdx.x / LANES;
-    const bool there = row_at < a.rows;
-    const int64_t row = there ? row_at : a.rows - 1;   // (lanes of a row that does not exist go along and store nothing)
-    const T* const x = a.x + row * a.ldx;
-    T* const y = a.y + row * a.ldy;
-    constexpr int UNROLL = CH ? CH : 1;
-    const int chunks = CH ? CH : (int)((a.k.pitch / 8 + LANES - 1) / LANES);
-    float v[CH ? CH : 1][8];
-    Raw8<T> raw[CH ? CH : 1];
-    auto count = [&](int c) { return max(0, min(8, a.cols - 8 * c)); };
-    if constexpr (CH != 0) {
+    const int64_t row0 = (int64_t)blockIdx.x * Group<LANES>::ROWS + threadIdx.x / LANES;
+    const bool there = row0 < a.rows;   // (lanes of a row that does not exist go along and store nothing)
+    int cols = a.cols;
+    auto count = [&](int i) { return max(0, min(8, cols - 8 * (j + i * LANES))); };
+    Raw8<T> raw[CH];
+    auto fetch = [&](int64_t row) {
+        const T* const x = a.x + row * a.ldx;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) raw[i] = row_chunk<RAGGED>(x, j + i * LANES, count(i));
+    };
+    int64_t row = there ? row0 : a.rows - 1;
+    fetch(row);
+    float w[MANY ? CH : 1][8], b[MANY ? CH : 1][8];
+    auto params = [&](int i, float* w, float* b) {
+        load_param<T>(a.weight, a.param_f32, 8 * (j + i * LANES), count(i), 1.0f, w);
+        load_param<T>(a.bias, a.param_f32, 8 * (j + i * LANES), count(i), 0.0f, b);
+    };
+    if constexpr (MANY)
+#pragma unroll
+        for (int i = 0; i < CH; ++i) params(i, w[i], b[i]);
+    for (;;) {
+        opaque_uniform(cols);   // (the masks of all chunks, kept from row to row, are more than there are scalar registers)
+        float v[CH][8], sum[1] = {0};
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const int c = j + i * LANES, n = count(c);
-            raw[i] = load_raw(x + 8 * c, n);
-        }
+            raw_values(raw[i], v[i]);
 #pragma unroll
-        for (int i = 0; i < CH; ++i) raw_values(raw[i], v[i]);
+            for (int u = 0; u < 8; ++u) sum[0] += v[i][u];
+        }
+        const int64_t next = row + gridDim.x;
+        if (MANY && next < a.rows) fetch(next);
+        group_sum<LANES, 1>(sum, red[0]);
+        const float mean = sum[0] * a.inv_cols;
+        sum[0] = 0;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int n = count(i);
+            if (n < 8) {   // columns that do not exist lie at the mean from here on
+#pragma unroll
+                for (int u = 0; u < 8; ++u) v[i][u] = RAGGED && u < n ? v[i][u] : mean;
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                v[i][u] -= mean;
+                sum[0] = __builtin_fmaf(v[i][u], v[i][u], sum[0]);
+            }
+        }
+        group_sum<LANES, 1>(sum, red[1]);
+        const float rstd = 1.0f / sqrtf(sum[0] * a.inv_cols + a.eps);
+        if (there && j == 0) {
+            if (a.mean) a.mean[row] = mean;
+            if (a.rstd) a.rstd[row] = rstd;
+        }
+        T* const y = a.y + row * a.ldy;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            opaque_uniform(cols);
+            const int c = j + i * LANES, n = count(i);
+            float h[8], o[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) h[u] = v[i][u] * rstd;
+            if constexpr (!MANY) params(i, w[0], b[0]);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) o[u] = __builtin_fmaf(h[u], w[MANY ? i : 0][u], b[MANY ? i : 0][u]);
+            row_store<RAGGED>(y, c, there ? n : 0, o);
+            if (a.k.q) {
+                const uint32_t m = quad_max_u32(abs_max_bits(h)), e = ckpt_exponent(m);
+                const u32x2 q = ckpt_codes(h, m, e, a.r, (uint64_t)row * (uint64_t)a.cols + 8 * (uint64_t)c);
+                if (there) ckpt_store_chunk(a.k, row, c, LANES * CH, n > 0, q, e);
+            }
+        }
+        if (!MANY || next >= a.rows) break;
+        row = next;
     }
-    auto values = [&](int i, int n) {   // CH == 0: the chunk is read again
-        if (CH == 0) load8(x + 8 * (j + i * LANES), n, v[0]);
-        return CH ? i : 0;
-    };
+}
+
+// Rows of more columns than a workgroup holds (32768): read three times, from the caches but for the first.
+template <typename T> __global__ __launch_bounds__(1024) void k_norm_forward_wide(NormForwardArgs<T> a)
+{
+    __shared__ float red[2][16];
+    const int64_t row = blockIdx.x;
+    const T* const x = a.x + row * a.ldx;
+    T* const y = a.y + row * a.ldy;
+    const int chunks = (int)(a.k.pitch / 8 + 1023) / 1024 * 1024;   // (pad columns of the checkpoint included, whole wavefronts)
     float sum[1] = {0};
-#pragma unroll UNROLL
-    for (int i = 0; i < chunks; ++i) {
-        const int at = values(i, count(j + i * LANES));
+    for (int c = threadIdx.x; c < chunks; c += 1024) {
+        float v[8];
+        load8(x + 8 * c, max(0, min(8, a.cols - 8 * c)), v);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) sum[0] += v[at][u];
+        for (int u = 0; u < 8; ++u) sum[0] += v[u];
     }
-    group_sum<LANES, 1>(sum, red[0]);
+    group_sum<1024, 1>(sum, red[0]);
     const float mean = sum[0] * a.inv_cols;
-    // columns that do not exist lie at the mean from here on
-    auto pad = [&](int at, int n) {
-        if (n < 8) {
+    auto deviations = [&](int c, float v[8]) {
+        const int n = max(0, min(8, a.cols - 8 * c));
+        load8(x + 8 * c, n, v);
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[at][u] = u < n ? v[at][u] : mean;
-        }
+        for (int u = 0; u < 8; ++u) v[u] = u < n ? v[u] - mean : mean - mean;
+        return n;
     };
     sum[0] = 0;
-#pragma unroll UNROLL
-    for (int i = 0; i < chunks; ++i) {
-        const int n = count(j + i * LANES), at = values(i, n);
-        pad(at, n);
+    for (int c = threadIdx.x; c < chunks; c += 1024) {
+        float v[8];
+        deviations(c, v);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const float d = v[at][u] - mean;
-            sum[0] = __builtin_fmaf(d, d, sum[0]);
-        }
+        for (int u = 0; u < 8; ++u) sum[0] = __builtin_fmaf(v[u], v[u], sum[0]);
     }
-    group_sum<LANES, 1>(sum, red[1]);
+    group_sum<1024, 1>(sum, red[1]);
     const float rstd = 1.0f / sqrtf(sum[0] * a.inv_cols + a.eps);
-    if (there && j == 0) {
+    if (threadIdx.x == 0) {
         if (a.mean) a.mean[row] = mean;
         if (a.rstd) a.rstd[row] = rstd;
     }
-#pragma unroll UNROLL
-    for (int i = 0; i < chunks; ++i) {
-        const int c = j + i * LANES, n = count(c), at = values(i, n);
-        if (CH == 0) pad(at, n);
-        float h[8];
+    for (int c = threadIdx.x; c < chunks; c += 1024) {
+        float h[8], w[8], b[8], o[8];
+        const int n = deviations(c, h);
+        load_param<T>(a.weight, a.param_f32, 8 * c, n, 1.0f, w);
+        load_param<T>(a.bias, a.param_f32, 8 * c, n, 0.0f, b);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) h[u] = (v[at][u] - mean) * rstd;
-        if (n > 0) {
-            float w[8], b[8], o[8];
-            load_param<T>(a.weight, a.param_f32, 8 * c, n, 1.0f, w);
-            load_param<T>(a.bias, a.param_f32, 8 * c, n, 0.0f, b);
-#pragma unroll
-            for (int u = 0; u < 8; ++u) o[u] = __builtin_fmaf(h[u], w[u], b[u]);
-            if (there) store8(y + 8 * c, n, o);
+        for (int u = 0; u < 8; ++u) {
+            h[u] *= rstd;
+            o[u] = __builtin_fmaf(h[u], w[u], b[u]);
         }
+        store8(y + 8 * c, n, o);
         if (a.k.q) {
             const uint32_t m = quad_max_u32(abs_max_bits(h)), e = ckpt_exponent(m);
             const u32x2 q = ckpt_codes(h, m, e, a.r, (uint64_t)row * (uint64_t)a.cols + 8 * (uint64_t)c);
-            if (there) ckpt_store_chunk(a.k, row, c, LANES * chunks, n > 0, q, e);
+            ckpt_store_chunk(a.k, row, c, chunks, n > 0, q, e);
         }
     }
 }
@@ -184,10 +258,10 @@ template <typename T> struct NormBackwardArgs {
     float2* row_sums;   // rows too wide for registers: both means of every row
 };
 
-// Rows a group has in flight.
-template <typename T, int CH> constexpr int rows_ahead() { return (sizeof(T) == 4 ? 2 : 4) / CH; }
+// Rows of a group in a round; the next round's are on their way meanwhile.
+template <typename T, int CH> constexpr int rows_ahead() { return sizeof(T) == 4 || CH > 1 ? 1 : 2; }
 
-template <typename T, bool KEPT, int LANES, int CH>
+template <typename T, bool KEPT, int LANES, int CH, bool RAGGED>
 __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_backward(NormBackwardArgs<T> a)
 {
     using G = Group<LANES>;
@@ -196,7 +270,8 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_backward(NormBac
     __shared__ __attribute__((aligned(16))) float cols_lds[G::ROWS > 1 ? G::THREADS * 16 : 4];
     const int j = threadIdx.x % LANES, group = threadIdx.x / LANES;
     const int64_t groups = (int64_t)gridDim.x * G::ROWS, g0 = (int64_t)blockIdx.x * G::ROWS + group;
-    auto count = [&](int i) { return max(0, min(8, a.cols - 8 * (j + i * LANES))); };
+    int cols = a.cols;
+    auto count = [&](int i) { return max(0, min(8, cols - 8 * (j + i * LANES))); };
     float w[CH][8], dw[CH][8], db[CH][8];
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
@@ -204,50 +279,57 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_backward(NormBac
         for (int u = 0; u < 8; ++u) dw[i][u] = db[i][u] = 0;
         load_param<T>(a.weight, a.param_f32, 8 * (j + i * LANES), count(i), 1.0f, w[i]);
     }
-    int phase = 0;
-    // every group of a workgroup of several wavefronts makes the same number of rounds: barriers are inside
-    const int64_t rounds = (a.rows + groups * R - 1) / (groups * R);
-    for (int64_t it = 0; it < rounds; ++it, phase ^= 1) {
-        Raw8<T> rd[R][CH];
-        std::conditional_t<KEPT, u32x2, Raw8<T>> rx[R][CH];
-        uint32_t re[R][CH];
+    struct Rows {
+        Raw8<T> d[R][CH];
+        std::conditional_t<KEPT, u32x2, Raw8<T>> x[R][CH];
+        uint32_t e[R][CH];
         float mean[R], rstd[R];
-        int64_t row[R];
-        bool there[R];
+    };
+    // Row k of round `it`; one that does not exist is the last row, with zeros for everything.
+    auto row_of = [&](int64_t it, int k) { return (it * R + k) * groups + g0; };
+    auto fetch = [&](int64_t it, Rows& to) {
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            row[k] = (it * R + k) * groups + g0;
-            there[k] = row[k] < a.rows;
-            if (!there[k]) row[k] = a.rows - 1;
+            const bool there = row_of(it, k) < a.rows;
+            const int64_t row = there ? row_of(it, k) : a.rows - 1;
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
-                const int c = j + i * LANES, n = there[k] ? count(i) : 0;
-                re[k][i] = 127;
+                const int c = j + i * LANES, n = there ? count(i) : 0;
                 if constexpr (KEPT) {
-                    rx[k][i] = u32x2{0, 0};
-                    if (n > 0) {
-                        rx[k][i] = *(const u32x2*)(a.k.q + row[k] * a.k.pitch + 8 * c);
-                        re[k][i] = a.k.e[row[k] * a.k.epitch + (c >> 2)];
-                    }
+                    const int at = n > 0 ? c : 0;
+                    const u32x2 q = *(const u32x2*)(a.k.q + row * a.k.pitch + 8 * at);
+                    const uint32_t e = a.k.e[row * a.k.epitch + (at >> 2)];
+                    to.x[k][i] = n > 0 ? q : u32x2{0, 0};
+                    to.e[k][i] = n > 0 ? e : 127u;
                 } else {
-                    rx[k][i] = load_raw(a.x + row[k] * a.ldx + 8 * c, n);
+                    to.x[k][i] = row_chunk<RAGGED>(a.x + row * a.ldx, c, n);
+                    to.e[k][i] = 0;
                 }
-                rd[k][i] = load_raw(a.dy + row[k] * a.lddy + 8 * c, n);
+                to.d[k][i] = row_chunk<RAGGED>(a.dy + row * a.lddy, c, n);
             }
-            // (a row that does not exist adds zeros, whatever the last row holds)
-            rstd[k] = there[k] ? a.rstd[row[k]] : 0.0f;
-            mean[k] = KEPT || !there[k] ? 0.0f : a.mean[row[k]];
+            const float rstd = a.rstd[row], mean = KEPT ? 0.0f : a.mean[row];
+            to.rstd[k] = there ? rstd : 0.0f;
+            to.mean[k] = there ? mean : 0.0f;
         }
-        auto rows_values = [&](int k, int i, float d[8], float h[8]) {
-            raw_values(rd[k][i], d);
-            if constexpr (KEPT) {
-                ckpt_values(rx[k][i], re[k][i], h);
-            } else {
-                raw_values(rx[k][i], h);
+    };
+    auto values = [&](const Rows& r, int k, int i, float d[8], float h[8]) {
+        raw_values(r.d[k][i], d);
+        if constexpr (KEPT) {
+            ckpt_values(r.x[k][i], r.e[k][i], h);
+        } else {
+            raw_values(r.x[k][i], h);
 #pragma unroll
-                for (int u = 0; u < 8; ++u) h[u] = (h[u] - mean[k]) * rstd[k];
-            }
-        };
+            for (int u = 0; u < 8; ++u) h[u] = (h[u] - r.mean[k]) * r.rstd[k];
+        }
+    };
+    // every group of a workgroup of several wavefronts makes the same number of rounds: barriers are inside
+    const int64_t rounds = (a.rows + groups * R - 1) / (groups * R);
+    Rows now, next;
+    fetch(0, next);
+    for (int64_t it = 0; it < rounds; ++it) {
+        opaque_uniform(cols);   // (see k_norm_forward)
+        now = next;
+        fetch(min(it + 1, rounds - 1), next);
         float s[2 * R];
 #pragma unroll
         for (int k = 0; k < R; ++k) {
@@ -256,7 +338,7 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_backward(NormBac
             for (int i = 0; i < CH; ++i) {
                 // (a column that does not exist has d = 0 and adds nothing, or a NaN where the row's own columns have them too)
                 float d[8], h[8];
-                rows_values(k, i, d, h);
+                values(now, k, i, d, h);
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
                     const float g = d[u] * w[i][u];
@@ -268,25 +350,25 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_backward(NormBac
             }
         }
         if (a.dx) {
-            group_sum<LANES, 2 * R>(s, red[phase]);
+            group_sum<LANES, 2 * R>(s, red[it & 1]);
 #pragma unroll
             for (int k = 0; k < R; ++k)
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {
-                    opaque(rd[k][i]);
-                    opaque(rx[k][i]);
+                    opaque(now.d[k][i]);
+                    opaque(now.x[k][i]);
                 }
 #pragma unroll
             for (int k = 0; k < R; ++k) {
                 const float c1 = s[2 * k] * a.inv_cols, c2 = s[2 * k + 1] * a.inv_cols;
+                const int64_t row = row_of(it, k);
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {
-                    const int c = j + i * LANES, n = there[k] ? count(i) : 0;
                     float d[8], h[8];
-                    rows_values(k, i, d, h);
+                    values(now, k, i, d, h);
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) d[u] = rstd[k] * (d[u] * w[i][u] - c1 - h[u] * c2);
-                    store8(a.dx + row[k] * a.lddx + 8 * c, n, d);
+                    for (int u = 0; u < 8; ++u) d[u] = now.rstd[k] * (d[u] * w[i][u] - c1 - h[u] * c2);
+                    row_store<RAGGED>(a.dx + row * a.lddx, j + i * LANES, row < a.rows ? count(i) : 0, d);
                 }
             }
         }
@@ -422,9 +504,11 @@ __global__ __launch_bounds__(256) void k_norm_columns(const float* part, int par
 // ------------------------------------------------------------------------------------------------
 template <typename T, int LANES, int CH> static hipError_t forward_as(const NormForwardArgs<T>& a, hipStream_t s)
 {
-    const int64_t wgs = (a.rows + Group<LANES>::ROWS - 1) / Group<LANES>::ROWS;
-    if (wgs > 0x7FFFFFFF) return hipErrorInvalidValue;   // (refused by the entry point)
-    k_norm_forward<T, LANES, CH><<<dim3((unsigned)wgs), Group<LANES>::THREADS, 0, s>>>(a);
+    // several wavefronts to a row: as many workgroups as run at once, each with its rows (16384 x 4096 bf16: 97 us with one row each, now 80)
+    const int64_t wgs = (a.rows + Group<LANES>::ROWS - 1) / Group<LANES>::ROWS, most = LANES > 64 && LANES < 1024 ? 256 * (1024 / LANES) : wgs;
+    const dim3 grid((unsigned)min(wgs, most));
+    if (a.cols % 8 == 0) k_norm_forward<T, LANES, CH, false><<<grid, Group<LANES>::THREADS, 0, s>>>(a);
+    else k_norm_forward<T, LANES, CH, true><<<grid, Group<LANES>::THREADS, 0, s>>>(a);
     return hipGetLastError();
 }
 template <typename T> static hipError_t forward_of(const NormForwardLaunch& l, hipStream_t s)
@@ -453,10 +537,11 @@ template <typename T> static hipError_t forward_of(const NormForwardLaunch& l, h
     if (chunks <= 64) return forward_as<T, 64, 1>(a, s);
     if (chunks <= 256) return forward_as<T, 256, 1>(a, s);
     if (chunks <= 512) return forward_as<T, 256, 2>(a, s);
-    if (chunks <= 1024) return forward_as<T, 256, 4>(a, s);
-    if (chunks <= 2048) return forward_as<T, 512, 4>(a, s);
+    if (chunks <= 1024) return forward_as<T, 512, 2>(a, s);
+    if (chunks <= 2048) return forward_as<T, 1024, 2>(a, s);
     if (chunks <= 4096) return forward_as<T, 1024, 4>(a, s);
-    return forward_as<T, 1024, 0>(a, s);
+    k_norm_forward_wide<T><<<dim3((unsigned)a.rows), 1024, 0, s>>>(a);
+    return hipGetLastError();
 }
 hipError_t launch_norm_forward(const NormForwardLaunch& a, hipStream_t s)
 {
@@ -495,6 +580,18 @@ size_t norm_backward_workspace(int64_t rows, int64_t cols)
     return n < FF_WS_MIN_BYTES ? FF_WS_MIN_BYTES : n;
 }
 
+template <typename T, bool KEPT, bool RAGGED> static void backward_as(const NormPlan& p, const NormBackwardArgs<T>& a, hipStream_t s)
+{
+    const dim3 grid((unsigned)p.wgs);
+    if (p.lanes == 4) k_norm_backward<T, KEPT, 4, 1, RAGGED><<<grid, 256, 0, s>>>(a);
+    else if (p.lanes == 8) k_norm_backward<T, KEPT, 8, 1, RAGGED><<<grid, 256, 0, s>>>(a);
+    else if (p.lanes == 16) k_norm_backward<T, KEPT, 16, 1, RAGGED><<<grid, 256, 0, s>>>(a);
+    else if (p.lanes == 32) k_norm_backward<T, KEPT, 32, 1, RAGGED><<<grid, 256, 0, s>>>(a);
+    else if (p.lanes == 64) k_norm_backward<T, KEPT, 64, 1, RAGGED><<<grid, 256, 0, s>>>(a);
+    else if (p.ch == 1) k_norm_backward<T, KEPT, 256, 1, RAGGED><<<grid, 256, 0, s>>>(a);
+    else if (p.lanes == 256) k_norm_backward<T, KEPT, 256, 2, RAGGED><<<grid, 256, 0, s>>>(a);
+    else k_norm_backward<T, KEPT, 512, 2, RAGGED><<<grid, 512, 0, s>>>(a);
+}
 template <typename T, bool KEPT> static hipError_t backward_of(const NormBackwardLaunch& l, hipStream_t s)
 {
     const NormPlan p = backward_plan(l.rows, l.cols);
@@ -517,27 +614,14 @@ template <typename T, bool KEPT> static hipError_t backward_of(const NormBackwar
     a.part = (float*)l.ws;
     a.pcols = padded_cols(l.cols);
     a.row_sums = (float2*)((char*)l.ws + align_up((size_t)(p.wgs * 2 * a.pcols) * sizeof(float), 256));
-    const dim3 grid((unsigned)p.wgs);
     if (l.rows > 0) {
         if (p.ch == 0) {
             if (a.dx) k_norm_row_sums<T, KEPT><<<dim3((unsigned)l.rows), 1024, 0, s>>>(a);
             k_norm_backward_wide<T, KEPT><<<dim3((unsigned)((a.cols + 2047) / 2048), (unsigned)p.wgs), 256, 0, s>>>(a);
-        } else if (p.lanes == 4) {
-            k_norm_backward<T, KEPT, 4, 1><<<grid, 256, 0, s>>>(a);
-        } else if (p.lanes == 8) {
-            k_norm_backward<T, KEPT, 8, 1><<<grid, 256, 0, s>>>(a);
-        } else if (p.lanes == 16) {
-            k_norm_backward<T, KEPT, 16, 1><<<grid, 256, 0, s>>>(a);
-        } else if (p.lanes == 32) {
-            k_norm_backward<T, KEPT, 32, 1><<<grid, 256, 0, s>>>(a);
-        } else if (p.lanes == 64) {
-            k_norm_backward<T, KEPT, 64, 1><<<grid, 256, 0, s>>>(a);
-        } else if (p.ch == 1) {
-            k_norm_backward<T, KEPT, 256, 1><<<grid, 256, 0, s>>>(a);
-        } else if (p.lanes == 256) {
-            k_norm_backward<T, KEPT, 256, 2><<<grid, 256, 0, s>>>(a);
+        } else if (a.cols % 8 == 0) {
+            backward_as<T, KEPT, false>(p, a, s);
         } else {
-            k_norm_backward<T, KEPT, 512, 2><<<grid, 512, 0, s>>>(a);
+            backward_as<T, KEPT, true>(p, a, s);
         }
         const hipError_t err = hipGetLastError();
         if (err != hipSuccess) return err;
