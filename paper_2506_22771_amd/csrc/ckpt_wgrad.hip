@@ -39,7 +39,7 @@ struct WgradArgs {
     int64_t rows;
     int32_t n, k, tiles_n, tiles_k, splits;
     int64_t steps, per;      // steps of all rows, steps of a split
-    int64_t plain;           // steps before this one are read without looking at the end of the matrix
+    int64_t plain;           // steps before this one are read with the range check alone
     const void* gamma;
     const void* beta;
     int32_t param_kind;      // type of gamma and beta
@@ -135,7 +135,7 @@ template <typename T, int BT, int WK> struct WgradTile {
     static constexpr int PIECES = SUB * P * TI;          // a wavefront's fragments of dy in a step, TJ matrix instructions each
     static constexpr int EVERY = PIECES / CH;            // pieces to a chunk
     // Steps on their way in registers: as many as a step's matrix instructions (32 clocks each) need to cover some 2500 clocks.
-    static constexpr int SETS = BT == 256 ? 2 : BT == 128 ? 4 : 6;
+    static constexpr int SETS = BT == 256 ? 2 : 4;
     // Fragments of dy read ahead: a read takes some 130 clocks and more, a piece 32 TJ of its SIMD's matrix pipe.
     static constexpr int AHEAD = PIECES < 3 ? 2 : BT == 256 ? 2 : 3;
     static constexpr int LDS = 3 * STAGE;
@@ -169,15 +169,17 @@ __global__ __launch_bounds__(128 * WK) __attribute__((amdgpu_waves_per_eu(BT == 
     const uint8_t* const ce = a.c.e + cb;
     struct Chunk { Raw8<T> d; u32x2 q; uint32_t e; };
     // Steps in order, from scalar bases and this thread's fixed offsets.  A chunk of dy may reach into the next row (n not a multiple of
-    // eight); that stays inside the matrix but for the last row.
+    // eight); words beyond the end of a matrix, rows that do not exist among them, fail the buffer's range check and are zero.
     const uint32_t off_d = (uint32_t)(r0 * a.lddy + cn) * sizeof(T), off_q = (uint32_t)(r0 * a.c.pitch + ck), off_e = (uint32_t)(r0 * a.c.epitch) + cb;
-    const char* base_d = (const char*)a.dy + step0 * S::BM * a.lddy * sizeof(T);
-    const char* base_q = (const char*)a.c.q + step0 * S::BM * a.c.pitch;
-    const char* base_e = (const char*)a.c.e + step0 * S::BM * a.c.epitch;
+    const int64_t step_d = S::BM * a.lddy * (int64_t)sizeof(T), step_q = S::BM * a.c.pitch, step_e = S::BM * a.c.epitch;
+    const char *base_d = (const char*)a.dy + step0 * step_d, *base_q = (const char*)a.c.q + step0 * step_q, *base_e = (const char*)a.c.e + step0 * step_e;
+    int64_t left_d = ((a.rows - 1) * a.lddy + a.n) * (int64_t)sizeof(T) - step0 * step_d;   // bytes up to the end
+    int64_t left_q = a.rows * a.c.pitch - step0 * step_q, left_e = a.rows * a.c.epitch - step0 * step_e;
+    auto buffer = [](const char* base, int64_t left) {
+        return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)min(left, (int64_t)0x7FFFFFFF), 0x00020000);
+    };
     auto fetch = [&](int i) {
-        const __amdgpu_buffer_rsrc_t bd = __builtin_amdgcn_make_buffer_rsrc((void*)base_d, 0, 0x7FFFFFFF, 0x00020000);
-        const __amdgpu_buffer_rsrc_t bq = __builtin_amdgcn_make_buffer_rsrc((void*)base_q, 0, 0x7FFFFFFF, 0x00020000);
-        const __amdgpu_buffer_rsrc_t be = __builtin_amdgcn_make_buffer_rsrc((void*)base_e, 0, 0x7FFFFFFF, 0x00020000);
+        const __amdgpu_buffer_rsrc_t bd = buffer(base_d, left_d), bq = buffer(base_q, left_q), be = buffer(base_e, left_e);
         const int at_d = (int)(i * S::ROWS * a.lddy * (int64_t)sizeof(T)), at_q = (int)(i * S::ROWS * a.c.pitch), at_e = (int)(i * S::ROWS * a.c.epitch);
         Chunk c;
         c.d.a = __builtin_amdgcn_raw_buffer_load_b128(bd, (int)off_d, at_d, 0);
@@ -187,9 +189,13 @@ __global__ __launch_bounds__(128 * WK) __attribute__((amdgpu_waves_per_eu(BT == 
         return c;
     };
     auto advance = [&](bool more) {   // to the next step, or not beyond the last (which is then fetched again and used by nobody)
-        base_d += more ? S::BM * a.lddy * (int64_t)sizeof(T) : 0;
-        base_q += more ? S::BM * a.c.pitch : 0;
-        base_e += more ? S::BM * a.c.epitch : 0;
+        const int64_t d = more ? step_d : 0, q = more ? step_q : 0, e = more ? step_e : 0;
+        base_d += d;
+        left_d -= d;
+        base_q += q;
+        left_q -= q;
+        base_e += e;
+        left_e -= e;
     };
     // Rows that do not exist are zero in both operands, columns beyond n too.
     auto fetch_last = [&](int64_t step, int i) {
@@ -216,6 +222,13 @@ __global__ __launch_bounds__(128 * WK) __attribute__((amdgpu_waves_per_eu(BT == 
         *(u32x4*)(at + S::P * S::PLANE) = x;
     };
 
+    float gamma[S::TJ], beta[S::TJ];   // of this lane's columns, asked for before the loop
+#pragma unroll
+    for (int j = 0; j < S::TJ; ++j) {
+        const int k = min(k0 + 32 * (wk * S::TJ + j) + lr, a.k - 1);
+        gamma[j] = param_at(a.gamma, a.param_kind, k, 1.0f);
+        beta[j] = param_at(a.beta, a.param_kind, k, 0.0f);
+    }
     v16f acc[S::TI][S::TJ];
     float db = 0;   // this lane's share of the sums of dy, for the tile wk % TI of its wavefront's rows n
 #pragma unroll
@@ -247,7 +260,7 @@ __global__ __launch_bounds__(128 * WK) __attribute__((amdgpu_waves_per_eu(BT == 
         asm volatile("" ::: "memory");
     };
 
-    const int64_t plain = min(step1, a.plain);   // steps read without looking at the end
+    const int64_t plain = min(step1, a.plain);
     if (step0 < plain) {
         constexpr int SETS = S::SETS;
         Chunk c[SETS][S::CH];
@@ -258,14 +271,15 @@ __global__ __launch_bounds__(128 * WK) __attribute__((amdgpu_waves_per_eu(BT == 
             advance(fetched + 1 < plain);
             ++fetched;
         };
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-            fetch_step(c[0]);
-#pragma unroll
-            for (int i = 0; i < S::CH; ++i) put(lds + st * S::STAGE, i, c[0][i]);
-        }
+        // The first steps are all asked for before any is waited for; two go to LDS and make room for two more.
 #pragma unroll
         for (int st = 0; st < SETS; ++st) fetch_step(c[st]);
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+#pragma unroll
+            for (int i = 0; i < S::CH; ++i) put(lds + st * S::STAGE, i, c[st][i]);
+            fetch_step(c[st]);
+        }
         meet();
         char *now = lds, *next = lds + S::STAGE, *after = lds + 2 * S::STAGE;
         v8bf fa[S::AHEAD], fb[S::TJ];
@@ -276,7 +290,7 @@ __global__ __launch_bounds__(128 * WK) __attribute__((amdgpu_waves_per_eu(BT == 
         v8bf fb_next[S::TJ];
         v8bf fs;
         auto work = [&](auto set) {
-            constexpr int ST = decltype(set)::value;
+            constexpr int ST = (decltype(set)::value + 2) % SETS;   // (the first two sets hold later steps than the others)
 #pragma unroll
             for (int piece = 0; piece < S::PIECES; ++piece) {
                 const int i = piece % S::TI, p = piece / S::TI % S::P, s = piece / (S::TI * S::P), chunk = piece / S::EVERY;
@@ -334,7 +348,7 @@ __global__ __launch_bounds__(128 * WK) __attribute__((amdgpu_waves_per_eu(BT == 
             if (step + decltype(st)::value < plain) work(st);
         });
     }
-    // what is left: the step with the last row, or all of them where a chunk may reach over several rows (n < 8)
+    // what is left: the step with the last row where that ends inside a word (the range check goes by words), or all of them where rows lie too far apart
     for (int64_t step = max(step0, plain); step < step1; ++step) {
         meet();
 #pragma nounroll
@@ -371,15 +385,14 @@ __global__ __launch_bounds__(128 * WK) __attribute__((amdgpu_waves_per_eu(BT == 
     for (int j = 0; j < S::TJ; ++j) {
         const int k = k0 + 32 * (wk * S::TJ + j) + lr;
         if (k >= a.k) continue;
-        const float g = param_at(a.gamma, a.param_kind, k, 1.0f), b = param_at(a.beta, a.param_kind, k, 0.0f);
 #pragma unroll
         for (int i = 0; i < S::TI; ++i)
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 const int nl = 32 * (wn * S::TI + i) + (v & 3) + 8 * (v >> 2) + 4 * lh, n = n0 + nl;
                 if (n >= a.n) continue;
-                float r = g * acc[i][j][v];
-                if (a.beta) r = __builtin_fmaf(b, sums[nl], r);
+                float r = gamma[j] * acc[i][j][v];
+                if (a.beta) r = __builtin_fmaf(beta[j], sums[nl], r);
                 float* const to = out + (int64_t)n * a.k + k;
                 *to = add ? *to + r : r;
             }
@@ -485,7 +498,7 @@ template <typename T> static hipError_t wgrad_of(const CkptWgradLaunch& l, hipSt
     a.per = p.per;
     const int bm = plan_rows(Terms<T>::N, p.tile);
     const bool near = bm * l.lddy * (int64_t)sizeof(T) < int64_t(1) << 30;   // (offsets inside a step are 32 bits)
-    a.plain = l.n < 8 || !near ? 0 : l.rows % bm == 0 && l.n % 8 == 0 ? p.steps : p.steps - 1;
+    a.plain = !near ? 0 : sizeof(T) == 2 && l.n % 2 != 0 ? p.steps - 1 : p.steps;
     a.gamma = l.gamma;
     a.beta = l.beta;
     a.param_kind = l.param_dtype;
