@@ -2,7 +2,7 @@
 
 Functions mirror the C-ABI names.  Tensor arguments are torch CUDA tensors (or None where the
 header allows NULL); their data_ptr() is handed to the library together with the current
-torch stream.  Nothing here computes."""
+torch stream.  The layer norm and checkpoint calls take the compiled way (csrc/bind.cpp).  Nothing here computes."""
 from __future__ import annotations
 
 import ctypes as C
@@ -301,65 +301,22 @@ def ff_train_step_at(net: Net, x_pos, x_neg, theta, lam, lr, seed, step_dev, adv
 
 
 # --- layer norm and 8-bit checkpoints.  Matrices are 2-D tensors of float32, bfloat16 or float16 with consecutive columns and any row
-# stride (a view of some columns of a wider tensor will do); shapes and types are compared with each other here, because the library
-# sees addresses and sizes only.
-_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+# stride (a view of some columns of a wider tensor will do).  Shapes, types, strides and devices are compared with each other (ValueError),
+# because the library sees addresses and sizes only; that and the marshalling are compiled (csrc/bind.cpp).
+_bind = None
 
 
-def _mat(t: torch.Tensor, what: str, rows: int, cols: int, dtype: torch.dtype):
-    """(address, row stride in elements) of a matrix."""
-    if t.dtype is not dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{what}: {dtype} [{rows}, {cols}] expected, got {t.dtype} {list(t.shape)}")
-    if not t.is_cuda:
-        raise ValueError(f"{what}: device tensor expected")
-    ld, step = t.stride()
-    if rows <= 1:
-        ld = max(ld, cols)
-    if (step != 1 and cols > 1) or ld < cols:
-        raise ValueError(f"{what}: consecutive columns and rows that do not overlap expected, got strides {[ld, step]}")
-    return t.data_ptr(), ld
-
-
-def _vec(t: Optional[torch.Tensor], what: str, n: int, dtype: torch.dtype) -> Optional[int]:
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.dim() != 1 or t.shape[0] != n:
-        raise ValueError(f"{what}: {dtype} [{n}] expected, got {t.dtype} {list(t.shape)}")
-    return _ptr(t)
-
-
-def _params(a: Optional[torch.Tensor], b: Optional[torch.Tensor], what: str, n: int, dtype: torch.dtype):
-    """(address, address, type) of a pair of parameter vectors, which are float32 or of the matrix's type."""
-    of = a.dtype if a is not None else b.dtype if b is not None else torch.float32
-    if of is not torch.float32 and of is not dtype:
-        raise ValueError(f"{what}: float32 or {dtype} expected, got {of}")
-    return _vec(a, what, n, of), _vec(b, what, n, of), _DTYPES[of]
-
-
-def _pitch(cols: int) -> int:   # ff_pitch, without the call
-    return (cols + 127) // 128 * 128 if cols > 512 else (cols + 15) // 16 * 16
-
-
-def _ckpt(q: Optional[torch.Tensor], e: Optional[torch.Tensor], rows: int, cols: int):
-    if q is None and e is None:
-        return None, None
-    if q is None or e is None:
-        raise ValueError("a checkpoint has both codes and exponent bytes")
-    want = (rows, _pitch(cols)), (rows, _pitch((cols + CKPT_BLOCK - 1) // CKPT_BLOCK))
-    if q.dtype is not torch.int8 or e.dtype is not torch.uint8 or q.shape != want[0] or e.shape != want[1]:
-        raise ValueError(f"checkpoint: int8 {list(want[0])} and uint8 {list(want[1])} expected, got {q.dtype} {list(q.shape)} and "
-                         f"{e.dtype} {list(e.shape)}")
-    return _ptr(q), _ptr(e)
-
-
-def _matrix_type(t: torch.Tensor, what: str) -> int:
-    if t.dim() != 2 or t.dtype not in _DTYPES:
-        raise ValueError(f"{what}: a float32, bfloat16 or float16 matrix expected, got {t.dtype} {list(t.shape)}")
-    return _DTYPES[t.dtype]
-
-
-def _ws(ws: Optional[torch.Tensor]):
-    return _ptr(ws), ws.numel() * ws.element_size() if ws is not None else 0
+def _native():
+    """The built marshalling module; raises if it has not been built (python -m paper_2506_22771_amd.build)."""
+    global _bind
+    if _bind is None:
+        lib()
+        try:
+            from . import _bind as module
+        except ImportError as e:
+            raise FileNotFoundError(f"paper_2506_22771_amd/_bind.so: {e}: build it with `python -m paper_2506_22771_amd.build`") from e
+        _bind = module
+    return _bind
 
 
 def ff_ckpt_blocks(cols: int) -> int:
@@ -374,12 +331,7 @@ def ckpt_empty(rows: int, cols: int, device="cuda"):
 
 def ff_layer_norm_forward(x, weight, bias, eps, y, mean, rstd, q=None, e=None, round_mode=ROUND_NEAREST, seed=0,
                           stream_tag=0) -> None:
-    kind, (rows, cols), of = _matrix_type(x, "x"), x.shape, x.dtype
-    (px, ldx), (py, ldy) = _mat(x, "x", rows, cols, of), _mat(y, "y", rows, cols, of)
-    pw, pb, pk = _params(weight, bias, "weight, bias", cols, of)
-    pq, pe = _ckpt(q, e, rows, cols)
-    _chk(lib().ff_layer_norm_forward(rows, cols, kind, pk, px, ldx, pw, pb, eps, py, ldy, _vec(mean, "mean", rows, torch.float32),
-                                     _vec(rstd, "rstd", rows, torch.float32), pq, pe, round_mode, seed, stream_tag, _stream()),
+    _chk(_native().layer_norm_forward(x, weight, bias, eps, y, mean, rstd, q, e, round_mode, seed, stream_tag, _stream()),
          "ff_layer_norm_forward")
 
 
@@ -389,41 +341,20 @@ def ff_layer_norm_workspace_bytes(rows: int, cols: int) -> int:
 
 def ff_layer_norm_backward(dy, x, mean, q, e, rstd, weight, dx, dweight, dbias, accumulate, ws) -> None:
     """h comes from x, mean and rstd, or, with x = None, from the checkpoint q, e and rstd."""
-    kind, (rows, cols), of = _matrix_type(dy, "dy"), dy.shape, dy.dtype
-    pdy, lddy = _mat(dy, "dy", rows, cols, of)
-    px, ldx = _mat(x, "x", rows, cols, of) if x is not None else (None, 0)
-    pdx, lddx = _mat(dx, "dx", rows, cols, of) if dx is not None else (None, 0)
-    pw, _, pk = _params(weight, None, "weight", cols, of)
-    pq, pe = _ckpt(q, e, rows, cols)
-    f32 = torch.float32
-    _chk(lib().ff_layer_norm_backward(rows, cols, kind, pk, pdy, lddy, px, ldx, _vec(mean, "mean", rows, f32), pq, pe,
-                                      _vec(rstd, "rstd", rows, f32), pw, pdx, lddx, _vec(dweight, "dweight", cols, f32),
-                                      _vec(dbias, "dbias", cols, f32), int(accumulate), *_ws(ws), _stream()),
+    _chk(_native().layer_norm_backward(dy, x, mean, q, e, rstd, weight, dx, dweight, dbias, accumulate, ws, _stream()),
          "ff_layer_norm_backward")
 
 
 def ff_ckpt_store(x, round_mode, seed, stream_tag, q, e) -> None:
-    kind, (rows, cols) = _matrix_type(x, "x"), x.shape
-    _chk(lib().ff_ckpt_store(*_typed_mat(x, "x", kind), rows, cols, round_mode, seed, stream_tag, *_ckpt(q, e, rows, cols), _stream()),
-         "ff_ckpt_store")
-
-
-def _typed_mat(t: torch.Tensor, what: str, kind: int):
-    p, ld = _mat(t, what, t.shape[0], t.shape[1], t.dtype)
-    return p, kind, ld
+    _chk(_native().ckpt_store(x, round_mode, seed, stream_tag, q, e, _stream()), "ff_ckpt_store")
 
 
 def ff_ckpt_load(q, e, x) -> None:
-    kind, (rows, cols) = _matrix_type(x, "x"), x.shape
-    _chk(lib().ff_ckpt_load(*_ckpt(q, e, rows, cols), rows, cols, *_typed_mat(x, "x", kind), _stream()), "ff_ckpt_load")
+    _chk(_native().ckpt_load(q, e, x, _stream()), "ff_ckpt_load")
 
 
 def ff_ckpt_act_backward(q, e, act, coeff, dy, dx) -> None:
-    kind, (rows, cols), of = _matrix_type(dx, "dx"), dx.shape, dx.dtype
-    pdx, lddx = _mat(dx, "dx", rows, cols, of)
-    pdy, lddy = _mat(dy, "dy", rows, cols, of) if dy is not None else (None, 0)
-    _chk(lib().ff_ckpt_act_backward(*_ckpt(q, e, rows, cols), rows, cols, act, _vec(coeff, "coeff", rows, torch.float32), pdy, lddy, pdx,
-                                    lddx, kind, _stream()), "ff_ckpt_act_backward")
+    _chk(_native().ckpt_act_backward(q, e, act, coeff, dy, dx, _stream()), "ff_ckpt_act_backward")
 
 
 def ff_ckpt_weight_grad_workspace_bytes(rows: int, n: int, k: int) -> int:
@@ -431,14 +362,7 @@ def ff_ckpt_weight_grad_workspace_bytes(rows: int, n: int, k: int) -> int:
 
 
 def ff_ckpt_weight_grad(dy, q, e, gamma, beta, dw, db, accumulate, ws) -> None:
-    kind, (rows, n) = _matrix_type(dy, "dy"), dy.shape
-    if dw.dim() != 2 or dw.shape[0] != n or dw.dtype is not torch.float32:
-        raise ValueError(f"dw: float32 [{n}, k] expected, got {dw.dtype} {list(dw.shape)}")
-    k = dw.shape[1]
-    pdy, lddy = _mat(dy, "dy", rows, n, dy.dtype)
-    pg, pb, pk = _params(gamma, beta, "gamma, beta", k, dy.dtype)
-    _chk(lib().ff_ckpt_weight_grad(pdy, kind, lddy, *_ckpt(q, e, rows, k), rows, n, k, pg, pb, pk, _ptr(dw),
-                                   _vec(db, "db", n, torch.float32), int(accumulate), *_ws(ws), _stream()), "ff_ckpt_weight_grad")
+    _chk(_native().ckpt_weight_grad(dy, q, e, gamma, beta, dw, db, accumulate, ws, _stream()), "ff_ckpt_weight_grad")
 
 
 KERNEL_CLASSES = ("gemm_fwd", "gemm_dw", "quant_act", "quant_grad", "quant_w", "update", "absmax", "small", "im2col",

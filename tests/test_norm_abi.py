@@ -111,21 +111,64 @@ def test_sizes_of_layouts_and_workspaces(ff):
     assert ff.ff_layer_norm_workspace_bytes(0, 4) >= ff.WS_MIN_BYTES
     assert ff.ff_ckpt_weight_grad_workspace_bytes(4, 0, 4) == 0 and ff.ff_ckpt_weight_grad_workspace_bytes(4, 65536, 4) == 0
     assert ff.ff_ckpt_weight_grad_workspace_bytes(1, 4, 4) >= ff.WS_MIN_BYTES
-    for cols in (1, 16, 500, 513, 784, 4096, 20000):
-        assert ff.binding._pitch(cols) == ff.ff_pitch(cols)
 
 
 def test_the_binding_compares_shapes_and_types(ff):
-    """Host tensors: every one of these is refused before the address is asked for, or because of where the tensor lies."""
+    """Every one of these is refused before the library is called.  Host tensors of the right shapes and types are refused for where they lie."""
     x, q, e = torch.zeros(4, 40), torch.zeros((4, 48), dtype=torch.int8), torch.zeros((4, 16), dtype=torch.uint8)
-    w = torch.zeros(40)
-    for bad in (lambda: ff.ff_layer_norm_forward(x, w, w, 1e-5, x[:3], None, None), lambda: ff.ff_layer_norm_forward(x.double(), w, w, 1e-5, x, None, None),
-                lambda: ff.ff_layer_norm_forward(x, w, w, 1e-5, x, None, None), lambda: ff.ff_layer_norm_forward(x[0], w, w, 1e-5, x, None, None),
-                lambda: ff.ff_ckpt_store(x, 0, 0, 0, q, e), lambda: ff.ff_ckpt_load(q, e, x.bool()),
-                lambda: ff.ff_ckpt_weight_grad(x, q, e, None, None, torch.zeros(39, 40), None, False, None),
-                lambda: ff.ff_ckpt_act_backward(q, e, 0, None, x.half(), x),
-                lambda: ff.binding._ckpt(q[:, :47], e, 4, 40), lambda: ff.binding._ckpt(q, e[:3], 4, 40), lambda: ff.binding._ckpt(q, None, 4, 40),
-                lambda: ff.binding._ckpt(q.to(torch.uint8), e, 4, 40), lambda: ff.binding._params(w.half(), None, "w", 40, torch.bfloat16),
-                lambda: ff.binding._params(w, w.half(), "w", 40, torch.float16), lambda: ff.binding._vec(w, "v", 39, torch.float32)):
-        with pytest.raises(ValueError):
+    w, r, none = torch.zeros(40), torch.zeros(4), None
+    ws = torch.zeros(1 << 16, dtype=torch.uint8)
+    matrix, device = "float32, bfloat16 or float16 matrix", "device tensor"
+    B = ff.binding._native()    # (the functions that take the stream as a number: there is none to ask for here)
+    for expected, bad in (
+            (matrix, lambda: B.layer_norm_forward(x.double(), w, w, 1e-5, x, r, r, none, none, 0, 0, 0, 0)),
+            (matrix, lambda: B.layer_norm_forward(x[0], w, w, 1e-5, x, r, r, none, none, 0, 0, 0, 0)),
+            ("x: a tensor", lambda: B.layer_norm_forward([1.0], w, w, 1e-5, x, r, r, none, none, 0, 0, 0, 0)),
+            ("x: a dense tensor", lambda: B.ckpt_store(x.to_sparse(), 0, 0, 0, q, e, 0)),
+            (device, lambda: B.layer_norm_forward(x, w, w, 1e-5, x, r, r, none, none, 0, 0, 0, 0)),
+            (matrix, lambda: B.ckpt_load(q, e, x.bool(), 0)),
+            (device, lambda: B.ckpt_store(x, 0, 0, 0, q, e, 0)),
+            (device, lambda: B.ckpt_act_backward(q, e, 0, none, none, x, 0)),
+            (device, lambda: B.layer_norm_backward(x, none, none, q, e, r, w, none, w, w, False, ws, 0)),
+            (device, lambda: B.ckpt_weight_grad(x, q, e, none, none, torch.zeros(40, 40), none, False, ws, 0))):
+        with pytest.raises(ValueError, match=expected):
             bad()
+    with pytest.raises(TypeError):
+        B.ckpt_load(q, e)
+
+
+@pytest.mark.gpu
+def test_the_binding_compares_device_tensors_with_each_other(ff):
+    new = lambda *shape, of=torch.float32: torch.zeros(shape, dtype=of, device="cuda")  # noqa: E731
+    x, w, r, none = new(4, 40), new(40), new(4), None
+    q, e = new(4, 48, of=torch.int8), new(4, 16, of=torch.uint8)
+    ws = new(1 << 20, of=torch.uint8)
+    forward = lambda x=x, w=w, b=w, y=x, m=r, r=r, q=none, e=none: ff.ff_layer_norm_forward(x, w, b, 1e-5, y, m, r, q, e)  # noqa: E731
+    wgrad = lambda dy=x, q=q, e=e, g=none, b=none, dw=new(40, 40), db=none, ws=ws: ff.ff_ckpt_weight_grad(dy, q, e, g, b, dw, db, False, ws)  # noqa: E731
+    backward = lambda dy=x, x=none, m=none, q=q, e=e, dx=none, dw=w: ff.ff_layer_norm_backward(dy, x, m, q, e, r, w, dx, dw, none, False, ws)  # noqa: E731
+    for expected, bad in (
+            (r"y: float32 \[4, 40\]", lambda: forward(y=x[:3])), (r"y: float32 \[4, 40\]", lambda: forward(y=x.half())),
+            ("consecutive columns", lambda: forward(x=new(40, 4).t(), y=x)), ("consecutive columns", lambda: forward(x=new(1, 40).expand(4, 40))),
+            (r"weight: float32 \[40\]", lambda: forward(w=new(39))), ("weight: float32", lambda: forward(w=w.half())),
+            (r"bias: float32 \[40\]", lambda: forward(b=w.bfloat16())), ("contiguous", lambda: forward(w=new(80)[::2])),
+            (r"mean: float32 \[4\]", lambda: forward(m=new(5))), (r"rstd: float32 \[4\]", lambda: forward(r=r.double())),
+            ("both codes and exponent bytes", lambda: forward(q=q)), (r"codes: contiguous int8 \[4, 48\]", lambda: forward(q=q[:, :47], e=e)),
+            (r"codes: contiguous int8 \[4, 48\]", lambda: forward(q=e, e=e)), (r"exponent bytes: contiguous uint8 \[4, 16\]", lambda: forward(q=q, e=e[:3])),
+            ("device tensor", lambda: forward(w=w.cpu())), ("device tensor", lambda: forward(q=q.cpu(), e=e)),
+            (r"x: float32 \[4, 40\]", lambda: backward(x=x[:, :39])), (r"dx: float32 \[4, 40\]", lambda: backward(dx=x.half())),
+            (r"dweight: float32 \[40\]", lambda: backward(dw=r)),
+            (r"dw: contiguous float32 \[40, 40\]", lambda: wgrad(dw=new(40, 40, of=torch.float16))), ("dw: contiguous", lambda: wgrad(dw=new(40, 80)[:, :40])),
+            ("dw: contiguous float32", lambda: wgrad(dw=new(39, 40))), (r"db: float32 \[40\]", lambda: wgrad(db=r)), ("gamma: float32", lambda: wgrad(g=w.half())),
+            ("ws: contiguous", lambda: wgrad(ws=ws[::2])), (r"codes: contiguous int8 \[4, 16\]", lambda: wgrad(dw=new(40, 9))),
+            (r"dy: float32 \[4, 40\]", lambda: ff.ff_ckpt_act_backward(q, e, 1, none, x.half(), x)),
+            (r"coeff: float32 \[4\]", lambda: ff.ff_ckpt_act_backward(q, e, 1, w, x, x))):
+        with pytest.raises(ValueError, match=expected):
+            bad()
+    # and the library's own refusals come back as its status
+    for status, bad in ((-1, lambda: ff.ff_ckpt_act_backward(q, e, 9, none, x, x)), (-1, lambda: ff.ff_ckpt_act_backward(q, e, 1, none, none, x)),
+                        (-4, lambda: wgrad(ws=ws[:16])), (-1, lambda: wgrad(ws=none)), (-1, lambda: backward(x=x)),
+                        (-1, lambda: ff.ff_ckpt_store(x, 7, 0, 0, q, e)), (-1, lambda: ff.ff_layer_norm_forward(x, w, w, -1.0, x, r, r)),
+                        (-2, lambda: ff.ff_layer_norm_forward(new(4, 0), none, none, 1e-5, new(4, 0), r, r))):
+        with pytest.raises(ff.FFError) as err:
+            bad()
+        assert err.value.status == status
