@@ -272,13 +272,35 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_backward(NormBac
     const int64_t groups = (int64_t)gridDim.x * G::ROWS, g0 = (int64_t)blockIdx.x * G::ROWS + group;
     int cols = a.cols;
     auto count = [&](int i) { return max(0, min(8, cols - 8 * (j + i * LANES))); };
-    float w[CH][8], dw[CH][8], db[CH][8];
+    // The weight is held in registers, or, where a lane has four chunks, in LDS: in memory its loads would wait for the next rows'.
+    constexpr bool HELD = CH < 4;
+    __shared__ __attribute__((aligned(16))) float w_lds[HELD ? 4 : LANES * CH * 8];
+    float held[HELD ? CH : 1][8], dw[CH][8], db[CH][8];
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
 #pragma unroll
         for (int u = 0; u < 8; ++u) dw[i][u] = db[i][u] = 0;
-        load_param<T>(a.weight, a.param_f32, 8 * (j + i * LANES), count(i), 1.0f, w[i]);
+        float* const w = held[HELD ? i : 0];
+        load_param<T>(a.weight, a.param_f32, 8 * (j + i * LANES), count(i), 1.0f, w);
+        if constexpr (!HELD) {   // (two planes of four floats a lane: neighbouring lanes in neighbouring banks)
+            ((f32x4*)w_lds)[(2 * i) * LANES + j] = f32x4{w[0], w[1], w[2], w[3]};
+            ((f32x4*)w_lds)[(2 * i + 1) * LANES + j] = f32x4{w[4], w[5], w[6], w[7]};
+        }
     }
+    auto weight = [&](int i, float w[8]) {   // (a lane reads what it wrote)
+        if constexpr (HELD) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) w[u] = held[i][u];
+        } else {
+            const f32x4 lo = ((const f32x4*)w_lds)[(2 * i) * LANES + j], hi = ((const f32x4*)w_lds)[(2 * i + 1) * LANES + j];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                w[u] = lo[u];
+                w[4 + u] = hi[u];
+            }
+        }
+    };
     struct Rows {
         Raw8<T> d[R][CH];
         std::conditional_t<KEPT, u32x2, Raw8<T>> x[R][CH];
@@ -324,12 +346,17 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_backward(NormBac
     };
     // every group of a workgroup of several wavefronts makes the same number of rounds: barriers are inside
     const int64_t rounds = (a.rows + groups * R - 1) / (groups * R);
+    constexpr bool AHEAD = CH < 4 || (sizeof(T) == 2 && (KEPT || !RAGGED));   // (the others of four chunks have no registers for a second row)
     Rows now, next;
-    fetch(0, next);
+    if constexpr (AHEAD) fetch(0, next);
     for (int64_t it = 0; it < rounds; ++it) {
         opaque_uniform(cols);   // (see k_norm_forward)
-        now = next;
-        fetch(min(it + 1, rounds - 1), next);
+        if constexpr (AHEAD) {
+            now = next;
+            fetch(min(it + 1, rounds - 1), next);
+        } else {
+            fetch(it, now);
+        }
         float s[2 * R];
 #pragma unroll
         for (int k = 0; k < R; ++k) {
@@ -337,16 +364,18 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_backward(NormBac
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
                 // (a column that does not exist has d = 0 and adds nothing, or a NaN where the row's own columns have them too)
-                float d[8], h[8];
+                float d[8], h[8], w[8];
                 values(now, k, i, d, h);
+                weight(i, w);
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
-                    const float g = d[u] * w[i][u];
+                    const float g = d[u] * w[u];
                     s[2 * k] += g;
                     s[2 * k + 1] = __builtin_fmaf(g, h[u], s[2 * k + 1]);
                     dw[i][u] = __builtin_fmaf(d[u], h[u], dw[i][u]);
                     db[i][u] += d[u];
                 }
+                if constexpr (CH == 4) __builtin_amdgcn_sched_barrier(0);   // (chunk by chunk: registers)
             }
         }
         if (a.dx) {
@@ -364,11 +393,13 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_backward(NormBac
                 const int64_t row = row_of(it, k);
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {
-                    float d[8], h[8];
+                    float d[8], h[8], w[8];
                     values(now, k, i, d, h);
+                    weight(i, w);
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) d[u] = now.rstd[k] * (d[u] * w[i][u] - c1 - h[u] * c2);
+                    for (int u = 0; u < 8; ++u) d[u] = now.rstd[k] * (d[u] * w[u] - c1 - h[u] * c2);
                     row_store<RAGGED>(a.dx + row * a.lddx, j + i * LANES, row < a.rows ? count(i) : 0, d);
+                    if constexpr (CH == 4) __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
@@ -563,7 +594,7 @@ static NormPlan backward_plan(int64_t rows, int64_t cols)
         for (p.lanes = 4; p.lanes < chunks; p.lanes *= 2) {}
     } else {
         p.lanes = chunks <= 512 ? 256 : 512;
-        p.ch = chunks <= 256 ? 1 : chunks <= 1024 ? 2 : 0;
+        p.ch = chunks <= 256 ? 1 : chunks <= 1024 ? 2 : chunks <= 2048 ? 4 : 0;
     }
     const int64_t per = p.lanes <= 64 ? 256 / p.lanes : 1;
     const int64_t most = p.ch == 0 ? 64 : p.lanes <= 64 ? 1024 : 512;
@@ -590,7 +621,8 @@ template <typename T, bool KEPT, bool RAGGED> static void backward_as(const Norm
     else if (p.lanes == 64) k_norm_backward<T, KEPT, 64, 1, RAGGED><<<grid, 256, 0, s>>>(a);
     else if (p.ch == 1) k_norm_backward<T, KEPT, 256, 1, RAGGED><<<grid, 256, 0, s>>>(a);
     else if (p.lanes == 256) k_norm_backward<T, KEPT, 256, 2, RAGGED><<<grid, 256, 0, s>>>(a);
-    else k_norm_backward<T, KEPT, 512, 2, RAGGED><<<grid, 512, 0, s>>>(a);
+    else if (p.ch == 2) k_norm_backward<T, KEPT, 512, 2, RAGGED><<<grid, 512, 0, s>>>(a);
+    else k_norm_backward<T, KEPT, 512, 4, RAGGED><<<grid, 512, 0, s>>>(a);
 }
 template <typename T, bool KEPT> static hipError_t backward_of(const NormBackwardLaunch& l, hipStream_t s)
 {
