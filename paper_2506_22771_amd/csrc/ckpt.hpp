@@ -177,10 +177,15 @@ __device__ __forceinline__ uint32_t quad_max_u32(uint32_t v)
 }
 __device__ __forceinline__ uint32_t abs_max_bits(const float v[8])
 {
-    uint32_t m = 0;
+    // bits have the order of the sizes: among values without a sign as signed integers, and among those with one as unsigned, above all others
+    int32_t p = 0;
+    uint32_t n = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    return m;
+    for (int i = 0; i < 8; ++i) {
+        p = max(p, __float_as_int(v[i]));
+        n = max(n, __float_as_uint(v[i]));
+    }
+    return max((uint32_t)p, n & 0x7FFFFFFFu);
 }
 // absmax = m * 2^E, 1 <= m < 2: s = E - 6, one more where m > 127/64, which is where adding 0x1FFFF carries into the exponent
 __device__ __forceinline__ uint32_t ckpt_exponent(uint32_t amax_bits)
@@ -210,11 +215,13 @@ __device__ __forceinline__ u32x2 ckpt_codes(const float v[8], uint32_t amax_bits
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = sr_head((lo + i) ^ (lo + i < lo ? k + c.key.k1 : k));
         }
+        // what sr_scale makes of t = v * inv, of t 2^24 = v 2^p: one product less
+        const int p = 151 - (int)e;
         uint32_t x[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float t = v[i] * inv;
-            x[i] = sr_top(sr_scale(t, sr_one_if_negative(t)), -SR_MOST, SR_MOST, w[i]);
+            const float t = -__builtin_amdgcn_ldexpf(v[i], p), one = __builtin_amdgcn_fmed3f(t * 0x1p127f, 0.0f, 1.0f);
+            x[i] = sr_top(__builtin_fmaf(one, 0x1p24f, __builtin_fmaf(one, -0x1p24f, t)), -SR_MOST, SR_MOST, w[i]);
         }
         q[0] = sr_pack(x[0], x[1], x[2], x[3]);
         q[1] = sr_pack(x[4], x[5], x[6], x[7]);

@@ -18,6 +18,13 @@ namespace ffi {
 template <int LANES> struct Group {
     static constexpr int THREADS = LANES <= 64 ? 256 : LANES;
     static constexpr int ROWS = THREADS / LANES;   // groups of a workgroup
+    // a lane's group; where a wavefront has one only, a scalar, and with it all addresses of its row
+    static __device__ __forceinline__ int mine()
+    {
+        if constexpr (ROWS == 1) return 0;
+        else if constexpr (LANES == 64) return __builtin_amdgcn_readfirstlane(threadIdx.x / LANES);
+        else return threadIdx.x / LANES;
+    }
 };
 
 // Sum over the lanes of a group, which every lane receives.  Groups of more than a wavefront meet in `red`, one word per wavefront
@@ -49,6 +56,14 @@ template <int LANES, int N> __device__ __forceinline__ void group_sum(float (&v)
             v[i] = t;
         }
     }
+}
+
+// 1 / sqrt(v) to one unit in the last place; the instruction takes no numbers below 2^-126.
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const bool low = v < 0x1p-96f;
+    const float r = __builtin_amdgcn_rsqf(low ? v * 0x1p96f : v);
+    return low ? r * 0x1p48f : r;
 }
 
 // Eight parameters of a chunk (n of them exist), in the element's type or in fp32; `none` where there are none.
@@ -106,8 +121,8 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForw
     constexpr bool MANY = LANES > 64 && LANES < 1024;   // (1024 lanes have no registers to spare)
     __shared__ float red[2][W];   // (a sum's words are written again behind the other sum's barrier)
     const int j = threadIdx.x % LANES;
-    const int64_t row0 = (int64_t)blockIdx.x * Group<LANES>::ROWS + threadIdx.x / LANES;
-    const bool there = row0 < a.rows;   // (lanes of a row that does not exist go along and store nothing)
+    const int64_t row0 = (int64_t)blockIdx.x * Group<LANES>::ROWS + Group<LANES>::mine();
+    const bool there = Group<LANES>::ROWS == 1 || row0 < a.rows;   // (lanes of a row that does not exist go along and store nothing)
     int cols = a.cols;
     auto count = [&](int i) { return max(0, min(8, cols - 8 * (j + i * LANES))); };
     Raw8<T> raw[CH];
@@ -154,7 +169,7 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForw
             }
         }
         group_sum<LANES, 1>(sum, red[1]);
-        const float rstd = 1.0f / sqrtf(sum[0] * a.inv_cols + a.eps);
+        const float rstd = inverse_root(sum[0] * a.inv_cols + a.eps);
         if (there && j == 0) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
@@ -214,7 +229,7 @@ template <typename T> __global__ __launch_bounds__(1024) void k_norm_forward_wid
         for (int u = 0; u < 8; ++u) sum[0] = __builtin_fmaf(v[u], v[u], sum[0]);
     }
     group_sum<1024, 1>(sum, red[1]);
-    const float rstd = 1.0f / sqrtf(sum[0] * a.inv_cols + a.eps);
+    const float rstd = inverse_root(sum[0] * a.inv_cols + a.eps);
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[row] = mean;
         if (a.rstd) a.rstd[row] = rstd;
@@ -268,7 +283,7 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_backward(NormBac
     constexpr int W = LANES > 64 ? LANES / 64 : 1, R = rows_ahead<T, CH>();
     __shared__ float red[2][2 * R * W];
     __shared__ __attribute__((aligned(16))) float cols_lds[G::ROWS > 1 ? G::THREADS * 16 : 4];
-    const int j = threadIdx.x % LANES, group = threadIdx.x / LANES;
+    const int j = threadIdx.x % LANES, group = G::mine();
     const int64_t groups = (int64_t)gridDim.x * G::ROWS, g0 = (int64_t)blockIdx.x * G::ROWS + group;
     int cols = a.cols;
     auto count = [&](int i) { return max(0, min(8, cols - 8 * (j + i * LANES))); };
