@@ -112,17 +112,22 @@ template <typename T> struct NormForwardArgs {
     CkptRound r;
 };
 
+// Groups that take row after row.  (Up to 64 chunks to a row, the next group's wavefronts hide as much: 65536 x 512 fp32 42 us, and 48 row after
+// row.  Four chunks of 1024 lanes leave no registers to spare.)
+constexpr bool many_rows(int lanes, int ch) { return lanes * ch > 64 && lanes * ch < 4096; }
+
 // CH chunks of a lane.  Workgroups of several wavefronts to a row take row after row, with the parameters in registers and the next row's values on
 // their way; the others take one row per group, whose few parameters the cache holds.
 template <typename T, int LANES, int CH, bool RAGGED>
 __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForwardArgs<T> a)
 {
     constexpr int W = LANES > 64 ? LANES / 64 : 1;
-    constexpr bool MANY = LANES > 64 && LANES < 1024;   // (1024 lanes have no registers to spare)
+    constexpr bool MANY = many_rows(LANES, CH);
     __shared__ float red[2][W];   // (a sum's words are written again behind the other sum's barrier)
     const int j = threadIdx.x % LANES;
     const int64_t row0 = (int64_t)blockIdx.x * Group<LANES>::ROWS + Group<LANES>::mine();
-    const bool there = Group<LANES>::ROWS == 1 || row0 < a.rows;   // (lanes of a row that does not exist go along and store nothing)
+    if (LANES == 64 && row0 >= a.rows) return;   // (a whole wavefront, which meets no other)
+    const bool there = Group<LANES>::ROWS == 1 || LANES == 64 || row0 < a.rows;   // (lanes of a row that does not exist go along and store nothing)
     int cols = a.cols;
     auto count = [&](int i) { return max(0, min(8, cols - 8 * (j + i * LANES))); };
     Raw8<T> raw[CH];
@@ -150,7 +155,7 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForw
 #pragma unroll
             for (int u = 0; u < 8; ++u) sum[0] += v[i][u];
         }
-        const int64_t next = row + gridDim.x;
+        const int64_t next = row + (int64_t)gridDim.x * Group<LANES>::ROWS;
         if (MANY && next < a.rows) fetch(next);
         group_sum<LANES, 1>(sum, red[0]);
         const float mean = sum[0] * a.inv_cols;
@@ -521,27 +526,35 @@ template <typename T, bool KEPT> __global__ __launch_bounds__(256) void k_norm_b
     }
 }
 
-// Adds the workgroups' column sums: 16 columns by 16 slices of the workgroups, then the slices in order.
-__global__ __launch_bounds__(256) void k_norm_columns(const float* part, int parts, int64_t pcols, int cols, float* dw, float* db,
-                                                      int accumulate)
+// Adds the workgroups' column sums: 32 columns (a cache line of fp32) by 64 slices of the workgroups, then the slices in order.
+__global__ __launch_bounds__(512) void k_norm_columns(const float* part, int parts, int64_t pcols, int cols, float* dw, float* db, int accumulate)
 {
-    __shared__ float red[16][17];
-    const int col = blockIdx.x * 16 + (threadIdx.x & 15), slice = threadIdx.x >> 4;
+    __shared__ float red[64][33], last[16][32];
+    const int lane = threadIdx.x & 7, slice = threadIdx.x >> 3, col = blockIdx.x * 32;
     float* const out = blockIdx.y ? db : dw;
     if (!out) return;
-    float v = 0;
-    if (col < cols) {
-        const float* const p = part + blockIdx.y * pcols + col;
+    float4 v = make_float4(0, 0, 0, 0);
+    if (col + 4 * lane < pcols) {   // (pcols is a multiple of eight)
+        const float* const p = part + blockIdx.y * pcols + col + 4 * lane;
 #pragma unroll 8
-        for (int g = slice; g < parts; g += 16) v += p[(int64_t)g * 2 * pcols];
+        for (int g = slice; g < parts; g += 64) {
+            const float4 t = *(const float4*)(p + (int64_t)g * 2 * pcols);
+            v = make_float4(v.x + t.x, v.y + t.y, v.z + t.z, v.w + t.w);
+        }
     }
-    red[slice][threadIdx.x & 15] = v;
+    red[slice][4 * lane] = v.x;
+    red[slice][4 * lane + 1] = v.y;
+    red[slice][4 * lane + 2] = v.z;
+    red[slice][4 * lane + 3] = v.w;
     __syncthreads();
-    if (slice == 0 && col < cols) {
-        v = 0;
+    const int c = threadIdx.x & 31, q = threadIdx.x >> 5;
+    last[q][c] = (red[4 * q][c] + red[4 * q + 1][c]) + (red[4 * q + 2][c] + red[4 * q + 3][c]);
+    __syncthreads();
+    if (threadIdx.x < 32 && col + c < cols) {
+        float sum = 0;
 #pragma unroll
-        for (int g = 0; g < 16; ++g) v += red[g][threadIdx.x];
-        out[col] = accumulate ? out[col] + v : v;
+        for (int g = 0; g < 16; ++g) sum += last[g][c];
+        out[col + c] = accumulate ? out[col + c] + sum : sum;
     }
 }
 
@@ -551,7 +564,7 @@ __global__ __launch_bounds__(256) void k_norm_columns(const float* part, int par
 template <typename T, int LANES, int CH> static hipError_t forward_as(const NormForwardArgs<T>& a, hipStream_t s)
 {
     // several wavefronts to a row: as many workgroups as run at once, each with its rows (16384 x 4096 bf16: 97 us with one row each, now 80)
-    const int64_t wgs = (a.rows + Group<LANES>::ROWS - 1) / Group<LANES>::ROWS, most = LANES > 64 && LANES < 1024 ? 256 * (1024 / LANES) : wgs;
+    const int64_t wgs = (a.rows + Group<LANES>::ROWS - 1) / Group<LANES>::ROWS, most = many_rows(LANES, CH) ? 256 * (1024 / Group<LANES>::THREADS) : wgs;
     const dim3 grid((unsigned)min(wgs, most));
     if (a.cols % 8 == 0) k_norm_forward<T, LANES, CH, false><<<grid, Group<LANES>::THREADS, 0, s>>>(a);
     else k_norm_forward<T, LANES, CH, true><<<grid, Group<LANES>::THREADS, 0, s>>>(a);
@@ -581,7 +594,8 @@ template <typename T> static hipError_t forward_of(const NormForwardLaunch& l, h
     if (chunks <= 16) return forward_as<T, 16, 1>(a, s);
     if (chunks <= 32) return forward_as<T, 32, 1>(a, s);
     if (chunks <= 64) return forward_as<T, 64, 1>(a, s);
-    if (chunks <= 256) return forward_as<T, 256, 1>(a, s);
+    if (chunks <= 128) return forward_as<T, 64, 2>(a, s);
+    if (chunks <= 256) return forward_as<T, 128, 2>(a, s);
     if (chunks <= 512) return forward_as<T, 256, 2>(a, s);
     if (chunks <= 1024) return forward_as<T, 512, 2>(a, s);
     if (chunks <= 2048) return forward_as<T, 1024, 2>(a, s);
@@ -604,15 +618,15 @@ static NormPlan backward_plan(int64_t rows, int64_t cols)
 {
     const int64_t chunks = (cols + 7) / 8;
     NormPlan p;
-    if (chunks <= 64) {
-        p.ch = 1;
-        for (p.lanes = 4; p.lanes < chunks; p.lanes *= 2) {}
+    if (chunks <= 128) {
+        p.ch = chunks <= 64 ? 1 : 2;
+        for (p.lanes = 4; p.lanes * p.ch < chunks; p.lanes *= 2) {}
     } else {
         p.lanes = chunks <= 512 ? 256 : 512;
         p.ch = chunks <= 256 ? 1 : chunks <= 1024 ? 2 : chunks <= 2048 ? 4 : 0;
     }
     const int64_t per = p.lanes <= 64 ? 256 / p.lanes : 1;
-    const int64_t most = p.ch == 0 ? 64 : p.lanes <= 64 ? 1024 : 512;
+    const int64_t most = p.ch == 0 ? 64 : p.lanes == 512 ? 256 : p.lanes <= 64 ? 1024 : 512;   // (of 512 lanes a compute unit holds one)
     const int64_t need = (rows + per - 1) / per;
     p.wgs = need < most ? need : most;
     return p;
@@ -633,7 +647,8 @@ template <typename T, bool KEPT, bool RAGGED> static void backward_as(const Norm
     else if (p.lanes == 8) k_norm_backward<T, KEPT, 8, 1, RAGGED><<<grid, 256, 0, s>>>(a);
     else if (p.lanes == 16) k_norm_backward<T, KEPT, 16, 1, RAGGED><<<grid, 256, 0, s>>>(a);
     else if (p.lanes == 32) k_norm_backward<T, KEPT, 32, 1, RAGGED><<<grid, 256, 0, s>>>(a);
-    else if (p.lanes == 64) k_norm_backward<T, KEPT, 64, 1, RAGGED><<<grid, 256, 0, s>>>(a);
+    else if (p.lanes == 64 && p.ch == 1) k_norm_backward<T, KEPT, 64, 1, RAGGED><<<grid, 256, 0, s>>>(a);
+    else if (p.lanes == 64) k_norm_backward<T, KEPT, 64, 2, RAGGED><<<grid, 256, 0, s>>>(a);
     else if (p.ch == 1) k_norm_backward<T, KEPT, 256, 1, RAGGED><<<grid, 256, 0, s>>>(a);
     else if (p.lanes == 256) k_norm_backward<T, KEPT, 256, 2, RAGGED><<<grid, 256, 0, s>>>(a);
     else if (p.ch == 2) k_norm_backward<T, KEPT, 512, 2, RAGGED><<<grid, 512, 0, s>>>(a);
@@ -674,8 +689,8 @@ template <typename T, bool KEPT> static hipError_t backward_of(const NormBackwar
         if (err != hipSuccess) return err;
     }
     if (a.sums) {
-        k_norm_columns<<<dim3((unsigned)((a.cols + 15) / 16), 2), 256, 0, s>>>(a.part, (int)p.wgs, a.pcols, a.cols, l.dweight, l.dbias,
-                                                                                l.accumulate);
+        k_norm_columns<<<dim3((unsigned)((a.cols + 31) / 32), 2), 512, 0, s>>>(a.part, l.rows > 0 ? (int)p.wgs : 0, a.pcols, a.cols, l.dweight,
+                                                                                l.dbias, l.accumulate);
         return hipGetLastError();
     }
     return hipSuccess;
