@@ -401,7 +401,8 @@ size_t ff_workspace_bytes(const ff_net_desc* net);
  * Matrices of floating-point values in this part
  *  - [rows, cols], element type `dtype` (FF_F32, FF_BF16 or FF_F16), consecutive columns, rows `ld` ELEMENTS apart,
  *    ld >= cols; base addresses aligned to the element.  Arithmetic is fp32 whatever the type; results are rounded once.
- *  - 1 <= cols <= 2^24 and 0 <= rows < 2^31 (FF_ERR_SHAPE / FF_ERR_UNSUPPORTED); no limit at 2^32 elements.
+ *  - 1 <= cols <= 2^24 and 0 <= rows < 2^31 (FF_ERR_SHAPE / FF_ERR_UNSUPPORTED); fewer than 2^34 elements, columns counted in whole
+ *    rows of codes (ff_pitch(cols), rounded up to whole blocks), else FF_ERR_UNSUPPORTED.
  *  - rows == 0 is accepted: matrix pointers may be NULL then, sums over rows are zero.
  *  - An output may be the very matrix of an input of the same shape and type (same base and ld); otherwise they must
  *    not overlap.

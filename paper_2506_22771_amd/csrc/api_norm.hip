@@ -11,8 +11,8 @@ static ff_status size_status(int64_t rows, int64_t cols)
     if (rows < 0 || cols < 0) return FF_ERR_INVALID_ARG;
     if (cols == 0) return FF_ERR_SHAPE;
     if (cols > MOST_COLS || rows > MOST_ROWS) return FF_ERR_UNSUPPORTED;
-    // one workgroup for at least 512 chunks of eight columns, fewer than 2^31 workgroups
-    if (rows * ((pitch8(cols) + 31) / 32 * 4) >= int64_t(1) << 40) return FF_ERR_UNSUPPORTED;
+    // chunks of eight columns, whole blocks of them; a launch has fewer than 2^32 lanes, at most two for a chunk
+    if (rows * ((pitch8(cols) + 31) / 32 * 4) >= int64_t(1) << 31) return FF_ERR_UNSUPPORTED;
     return FF_OK;
 }
 static bool type_ok(int32_t t) { return t == FF_F32 || t == FF_BF16 || t == FF_F16; }

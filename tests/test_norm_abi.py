@@ -172,3 +172,14 @@ def test_the_binding_compares_device_tensors_with_each_other(ff):
         with pytest.raises(ff.FFError) as err:
             bad()
         assert err.value.status == status
+
+
+@pytest.mark.parametrize("rows, cols", [(1 << 27, 1024), ((1 << 26) - 1, 257), (1 << 29, 1)])
+def test_more_elements_than_a_launch_has_lanes_for(ff, rows, cols):
+    """Refused, not handed to a launch that fails: 2^34 elements of rows of codes and more (257 columns: rows of 272 codes, 288 with whole blocks)."""
+    L = ff.lib()
+    for fn, args in ((L.ff_layer_norm_forward, FORWARD), (L.ff_layer_norm_backward, BACKWARD), (L.ff_ckpt_store, STORE), (L.ff_ckpt_load, LOAD),
+                     (L.ff_ckpt_act_backward, ACT)):
+        assert call(fn, args, rows=rows, cols=cols) == UNSUPPORTED
+    assert ff.ff_layer_norm_workspace_bytes(rows, cols) == 0
+    assert ff.ff_layer_norm_workspace_bytes((1 << 24) - 1, 1000) > 0
