@@ -8,6 +8,15 @@
 //
 // Both are bound by memory: a row is read once and held in registers by a group of 4 to 1024 lanes, eight columns (a chunk) of a lane
 // at a time.  The forward pass can write the checkpoint of h beside y, and the backward pass reads h from it (1.03 bytes a value) instead of x.
+//
+// Measured, us and TB/s (a copy of as many bytes reaches 5.3):
+//                                    16384 x 4096 bf16    16384 x 4096 fp32    131072 x 784 bf16    262144 x 128 fp16
+//   forward                              45   6.0              98   5.4              82   5.0              23   5.9
+//   forward, codes to nearest            62   5.4             113   5.4             111   4.6              30   5.7
+//   forward, stochastic codes         67-77   4.7             115   5.3             130   4.0              44   3.8
+//   backward from x                      81   5.0             156   5.1             146   4.2              41   5.0
+//   backward from the checkpoint      70-81   4.5             118   5.1             135   3.8              36   4.7
+// Stochastic codes of 16-bit values are as much arithmetic as memory: some 30 operations a value, of which the random word takes ten.
 #include <type_traits>
 
 #include "ckpt.hpp"
@@ -146,8 +155,8 @@ template <typename T> struct NormForwardArgs {
 // row.  Four chunks of 1024 lanes leave no registers to spare.)
 constexpr bool many_rows(int lanes, int ch) { return lanes * ch > 64 && lanes * ch < 4096; }
 
-// CH chunks of a lane.  Workgroups of several wavefronts to a row take row after row, with the parameters in registers and the next row's values on
-// their way; the others take one row per group, whose few parameters the cache holds.
+// CH chunks of a lane.  Groups that take row after row keep the parameters in registers and have the next row's values on their way; the others take
+// one row each, whose few parameters the cache holds.
 template <typename T, int LANES, int CH, bool RAGGED>
 __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForwardArgs<T> a)
 {
@@ -597,7 +606,8 @@ __global__ __launch_bounds__(512) void k_norm_columns(const float* part, int par
 // ------------------------------------------------------------------------------------------------
 template <typename T, int LANES, int CH> static hipError_t forward_as(const NormForwardArgs<T>& a, hipStream_t s)
 {
-    // several wavefronts to a row: as many workgroups as run at once, each with its rows (16384 x 4096 bf16: 97 us with one row each, now 80)
+    // row after row: as many workgroups as run at once (16384 x 4096 bf16 with stochastic codes, both before the codes' arithmetic was cut: 97 us with one
+    // row each, 80 row after row)
     const int64_t wgs = (a.rows + Group<LANES>::ROWS - 1) / Group<LANES>::ROWS, most = many_rows(LANES, CH) ? 256 * (1024 / Group<LANES>::THREADS) : wgs;
     const dim3 grid((unsigned)min(wgs, most));
     if (a.cols % 8 == 0) k_norm_forward<T, LANES, CH, false><<<grid, Group<LANES>::THREADS, 0, s>>>(a);
@@ -622,6 +632,9 @@ template <typename T> static hipError_t forward_of(const NormForwardLaunch& l, h
     a.inv_cols = 1.0f / (float)l.cols;
     a.k = ckpt_ptr(l.q, l.e, l.cols);
     a.r = {make_sr_key(l.seed, l.tag), l.round_mode == FF_ROUND_STOCHASTIC};
+    // Lanes of a row: as few as hold it in two chunks each, since a wavefront's own sums need no barrier and fewer lanes are left over (131072 x 784
+    // bf16, stochastic codes: 359 us by 256 lanes with a chunk each, 129 by 64; 32768 x 2000: 101 by 256, 74 by 128), and the smallest power of two for
+    // one chunk below that.
     const int64_t chunks = (a.k.pitch / 8 + 3) / 4 * 4;   // (pad columns of the checkpoint included)
     if (chunks <= 4) return forward_as<T, 4, 1>(a, s);
     if (chunks <= 8) return forward_as<T, 8, 1>(a, s);
@@ -643,7 +656,9 @@ hipError_t launch_norm_forward(const NormForwardLaunch& a, hipStream_t s)
     return a.dtype == FF_F32 ? forward_of<float>(a, s) : a.dtype == FF_BF16 ? forward_of<bf16_t>(a, s) : forward_of<f16_t>(a, s);
 }
 
-// Lanes of a row and workgroups of the backward pass.
+// Lanes of a row and workgroups of the backward pass: as many as run at once, each with a share of the rows and one set of column sums.  Up to 1024
+// columns a wavefront has a row to itself (131072 x 784 bf16: 237 us by 256 lanes with a chunk each, 144 by 64 with two); of 1025 to 2048, 256 lanes with
+// one chunk leave more registers for rows ahead than 128 with two.
 struct NormPlan {
     int lanes, ch;   // ch == 0: rows too wide for registers
     int64_t wgs;     // workgroups that leave column sums
