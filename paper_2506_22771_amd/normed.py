@@ -134,15 +134,15 @@ class NormedNet:
             ff.ff_ckpt_act_backward(*s.u, ff.ACT_RELU, s.coeff, None if down is None else down * lam, g)
             ff.ff_ckpt_weight_grad(g, *s.h, self.gamma[i], self.beta[i], self.grad.weight[i], None, accumulate, self.ws)
             dy = self._through_weights(i, g, ff.ff_stream_tag(step, i, p, ff.KIND_GRAD))
-            ff.ff_layer_norm_backward(dy, None, None, *s.h, s.rstd, self.gamma[i], None, self.grad.gamma[i], self.grad.beta[i], accumulate, self.ws)
-            if lam == 0.0 or i == 0:
-                down = None
-                continue
-            if down is not None and lam != 1.0:     # what the layers below get of the ones above is not scaled twice
+            grads = self.grad.gamma[i], self.grad.beta[i]
+            below = None if lam == 0.0 or i == 0 else torch.empty((self.batch, K), device=dy.device)
+            alike = down is None or lam == 1.0      # g is t as well: what the layers below get of the ones above is not scaled twice
+            ff.ff_layer_norm_backward(dy, None, None, *s.h, s.rstd, self.gamma[i], below if alike else None, *grads, accumulate, self.ws)
+            if below is not None and not alike:
                 ff.ff_ckpt_act_backward(*s.u, ff.ACT_RELU, s.coeff, down, g)
                 dy = self._through_weights(i, g, ff.ff_stream_tag(step, i, p, KIND_DOWN))
-            down = torch.empty((self.batch, K), device=dy.device)
-            ff.ff_layer_norm_backward(dy, None, None, *s.h, s.rstd, self.gamma[i], down, None, None, False, self.ws)
+                ff.ff_layer_norm_backward(dy, None, None, *s.h, s.rstd, self.gamma[i], below, None, None, False, self.ws)
+            down = below
         return self.grad
 
     def step(self, x_pos: torch.Tensor, x_neg: torch.Tensor, lam: float, lr: float, step: int = 0) -> torch.Tensor:
