@@ -285,3 +285,36 @@ def test_calls_in_a_graph():
         torch.cuda.synchronize()
         step()
         assert all(torch.equal(a, b) for a, b in zip(got, (y, dx, gw, gb, dW, dB)))
+
+
+# More rows than groups run at once, so that they go row after row, at every group that does: 64 lanes (1024 workgroups of four rows), 128 (2048 workgroups) to
+# 1024 (256), and the backward pass' few workgroups; whole chunks and rows that end inside one
+LONG = [(4400, 784, "float32"), (4200, 1001, "bfloat16"), (2200, 1500, "float16"), (1200, 3001, "float32"), (600, 6002, "bfloat16"), (300, 12001, "float16"),
+        (260, 16384, "bfloat16")]
+
+
+@pytest.mark.parametrize("rows, cols, dtype", LONG)
+def test_row_after_row(rows, cols, dtype):
+    test_forward(rows, cols, dtype)
+    test_backward(rows, cols, dtype)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("rows, cols", [(70, 6), (65, 33), (33, 100), (9, 500), (4200, 1001), (2200, 1500), (300, 12001), (3, 33001)])
+def test_in_place(rows, cols, dtype):
+    """A row that ends inside a chunk is read by two lanes in part; all of it before any of it is written."""
+    x, dy, w, b = inputs(rows, cols, dtype)
+    w, b = typed(w, "float32"), typed(b, "float32")
+    m, r, y = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty_like(x)
+    ff.ff_layer_norm_forward(x, w, b, EPS, y, m, r)
+    q, e = ff.ckpt_empty(rows, cols)
+    q2, e2 = ff.ckpt_empty(rows, cols)
+    ff.ff_layer_norm_forward(x, w, b, EPS, torch.empty_like(x), m, r, q, e, ff.ROUND_STOCHASTIC, 1, 2)
+    dx = torch.empty_like(x)
+    run_backward(dy, x, m, None, None, r, w, dx)
+    over_x, over_dy = x.clone(), dy.clone()
+    run_backward(dy, over_x, m, None, None, r, w, over_x)
+    run_backward(over_dy, x, m, None, None, r, w, over_dy)
+    assert torch.equal(over_x, dx) and torch.equal(over_dy, dx)
+    ff.ff_layer_norm_forward(x, w, b, EPS, x, m, r, q2, e2, ff.ROUND_STOCHASTIC, 1, 2)
+    assert torch.equal(x, y) and torch.equal(q, q2) and torch.equal(e, e2)
