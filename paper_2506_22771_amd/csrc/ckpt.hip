@@ -5,10 +5,10 @@
 //                  G = sum f(u)^2 of Section III (dL/dG = c), dy what comes down from the layers above (either may be absent)
 //
 // Measured, us and TB/s, 16384 x 4096 (a copy of as many bytes reaches 5.3): bf16 store 31 (6.5), with stochastic rounding 45-49 (4.2, by its arithmetic:
-// 25 operations a value), load 30 (6.8), GELU backward 75 (4.5); fp32 60 (5.6), 63 (5.4), 73 (4.6), 110 (5.5).
+// 25 operations a value), load 30 (6.8), GELU backward 65 (5.2); fp32 60 (5.6), 63 (5.4), 71 (4.8), 110 (5.5).
 // All three are bound by memory but for that.  A lane has eight columns (a chunk) of a row, a quad of lanes one block; a workgroup takes consecutive chunks,
 // whatever the row length, and has all its loads in flight before the first is used.
-#include <math.h>
+#include <type_traits>
 
 #include "ckpt.hpp"
 #include "norm.hpp"
@@ -59,7 +59,17 @@ template <typename T> struct CkptArgs {
     int32_t cols, act;
 };
 
-template <typename T, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckpt_store(CkptArgs<T> a)
+// A chunk `at` chunks behind the workgroup's first one: its place (that of the matrix' first where there is none) and how many of its columns exist.
+__device__ __forceinline__ int chunk_at(const Chunks& c, int cols, int64_t first, int64_t row0, uint32_t chunk0, uint32_t at, int64_t& row, uint32_t& chunk)
+{
+    chunk_place(c, row0, chunk0, at, row, chunk);
+    const bool there = first + at < c.total;
+    row = there ? row : 0;
+    chunk = there ? chunk : 0;
+    return there ? max(0, min(8, cols - 8 * (int)chunk)) : 0;
+}
+
+template <typename T, RowEnds ENDS, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckpt_store(CkptArgs<T> a)
 {
     const int64_t first = (int64_t)blockIdx.x * (CK_THREADS * U);
     int64_t row0;
@@ -71,14 +81,13 @@ template <typename T, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckp
     int n[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-        const uint32_t at = i * CK_THREADS + threadIdx.x;
-        chunk_place(a.c, row0, chunk0, at, row[i], chunk[i]);
-        n[i] = first + at < a.c.total ? min(8, a.cols - 8 * (int)chunk[i]) : 0;   // (at most 0: no columns of x)
-        raw[i] = load_raw(a.in + row[i] * a.ld_in + 8 * chunk[i], max(0, n[i]));
+        n[i] = chunk_at(a.c, a.cols, first, row0, chunk0, i * CK_THREADS + threadIdx.x, row[i], chunk[i]);
+        raw[i] = row_chunk<ENDS>(a.in + row[i] * a.ld_in, (int)chunk[i], n[i], a.cols);
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         float v[8];
+        settle<ENDS>(raw[i], n[i], a.cols);
         raw_values(raw[i], v);
         const uint32_t m = quad_max_u32(abs_max_bits(v)), e = ckpt_exponent(m);
         const u32x2 q = ckpt_codes(v, m, e, a.r, (uint64_t)row[i] * (uint64_t)a.cols + 8 * (uint64_t)chunk[i]);
@@ -90,6 +99,7 @@ template <typename T, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckp
 template <typename T> __device__ __forceinline__ float ckpt_clamp(float v) { return v; }
 template <> __device__ __forceinline__ float ckpt_clamp<f16_t>(float v) { return v == v ? __builtin_amdgcn_fmed3f(v, -65504.0f, 65504.0f) : v; }
 
+// (Its loads are behind branches, one chunk's after the other's: all at once, 16384 x 4096 fp32 values took 80 us in the place of 71.)
 template <typename T, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckpt_load(CkptArgs<T> a)
 {
     const int64_t first = (int64_t)blockIdx.x * (CK_THREADS * U);
@@ -126,8 +136,8 @@ template <typename T, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckp
 }
 
 // f(u) and f'(u).  GELU: Phi(-|u|) = 1/2 t (a1 + t (a2 + ...)) exp(-u^2/2), t = 1 / (1 + p |u| / sqrt 2): Abramowitz and Stegun 7.1.26, off by at
-// most 0.75e-7 (about one unit of fp32 at 1), and its exponential is the density's too.  With the library's erf and exp the large case below was bound by
-// vector arithmetic: 16384 x 4096 bf16 values 96 us, 75 this way.
+// most 0.75e-7 (about one unit of fp32 at 1), and its exponential is the density's too.  The large case below is bound by vector arithmetic before it is bound by
+// memory: 16384 x 4096 bf16 values 96 us with the library's erf and exp, 65 this way (75 with loads behind branches and six operations a value more).
 template <int ACT> __device__ __forceinline__ void act_of(float u, float& f, float& d)
 {
     if constexpr (ACT == FF_ACT_RELU) {
@@ -136,11 +146,12 @@ template <int ACT> __device__ __forceinline__ void act_of(float u, float& f, flo
     } else if constexpr (ACT == FF_ACT_GELU) {
         const float e = __builtin_amdgcn_exp2f(u * u * -0.72134752044448170f);              // exp(-u^2 / 2)
         const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(u), 0.23164189110f, 1.0f));   // p / sqrt 2
-        float q = __builtin_fmaf(t, 1.061405429f, -1.453152027f);
-        q = __builtin_fmaf(t, q, 1.421413741f);
-        q = __builtin_fmaf(t, q, -0.284496736f);
-        q = __builtin_fmaf(t, q, 0.254829592f);
-        const float low = 0.5f * t * q * e, phi = u >= 0.0f ? 1.0f - low : low;   // (u NaN: e is, and low)
+        float q = __builtin_fmaf(t, 0.5307027145f, -0.7265760135f);                         // half of the polynomial
+        q = __builtin_fmaf(t, q, 0.7107068705f);
+        q = __builtin_fmaf(t, q, -0.142248368f);
+        q = __builtin_fmaf(t, q, 0.127414796f);
+        // Phi(u): 1 - low above zero, else low; a code that is not zero stands for 2^-106 at least
+        const float phi = __builtin_fabsf(__builtin_amdgcn_fmed3f(u * 0x1p127f, 0.0f, 1.0f) - t * q * e);
         f = u * phi;
         d = __builtin_fmaf(u * e, 0.39894228040143268f, phi);
     } else if constexpr (ACT == FF_ACT_SILU) {
@@ -153,47 +164,48 @@ template <int ACT> __device__ __forceinline__ void act_of(float u, float& f, flo
     }
 }
 
-template <typename T, int ACT, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckpt_act_backward(CkptArgs<T> a)
+template <typename T, int ACT, RowEnds ENDS, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckpt_act_backward(CkptArgs<T> a)
 {
     const int64_t first = (int64_t)blockIdx.x * (CK_THREADS * U);
     int64_t row0;
     uint32_t chunk0;
     chunk_first(a.c, first, row0, chunk0);
+    // dy or c that is not there is zero: its loads all go to one place that is there, and count for nothing
+    const T* const in = a.in ? a.in : a.out;
+    const int64_t ld_in = a.in ? a.ld_in : 0, ld_c = a.coeff ? 1 : 0;
+    const float* const coeff = a.coeff ? a.coeff : (const float*)a.k.q;
+    const uint32_t c_mask = a.coeff ? 0xFFFFFFFFu : 0u;
     Raw8<T> raw[U];
     u32x2 q[U];
     uint32_t e[U];
-    float c2[U];
+    float c[U];
     T* to[U];
     int n[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-        const uint32_t at = i * CK_THREADS + threadIdx.x;
         int64_t row;
         uint32_t chunk;
-        chunk_place(a.c, row0, chunk0, at, row, chunk);
-        n[i] = first + at < a.c.total ? min(8, a.cols - 8 * (int)chunk) : 0;
+        n[i] = chunk_at(a.c, a.cols, first, row0, chunk0, i * CK_THREADS + threadIdx.x, row, chunk);
         to[i] = a.out + row * a.ld_out + 8 * chunk;
-        raw_zero(raw[i]);
-        q[i] = u32x2{0, 0};
-        e[i] = 127;
-        c2[i] = 0;
-        if (n[i] > 0) {
-            if (a.in) raw[i] = load_raw(a.in + row * a.ld_in + 8 * chunk, n[i]);
-            q[i] = *(const u32x2*)(a.k.q + row * a.k.pitch + 8 * chunk);
-            e[i] = a.k.e[row * a.k.epitch + (chunk >> 2)];
-            if (a.coeff) c2[i] = 2.0f * a.coeff[row];
-        }
+        raw[i] = row_chunk<ENDS>(in + row * ld_in, (int)chunk, a.in ? n[i] : 0, a.cols);
+        chunk = n[i] > 0 ? chunk : 0;   // (the row's pitch ends before its last block)
+        q[i] = *(const u32x2*)(a.k.q + row * a.k.pitch + 8 * chunk);
+        e[i] = a.k.e[row * a.k.epitch + (chunk >> 2)];
+        c[i] = coeff[row * ld_c];
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         float u[8], v[8];
+        settle<ENDS>(raw[i], a.in ? n[i] : 0, a.cols);
+        const float c2 = 2.0f * __uint_as_float(__float_as_uint(c[i]) & c_mask);
         ckpt_values(q[i], e[i], u);
         raw_values(raw[i], v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             float f, d;
             act_of<ACT>(u[j], f, d);
-            v[j] = (a.coeff ? __builtin_fmaf(c2[i], f, v[j]) : v[j]) * d;
+            // (c2 = 0 where there is no c: f is finite, or it is NaN and so is d, but for the identity's)
+            v[j] = ACT == FF_ACT_IDENTITY && !a.coeff ? v[j] : __builtin_fmaf(c2, f, v[j]) * d;
         }
         if (n[i] > 0) store8(to[i], n[i], v);
     }
@@ -210,6 +222,12 @@ template <typename T> static CkptArgs<T> ckpt_args(const int8_t* q, const uint8_
     a.cols = (int32_t)cols;
     return a;
 }
+template <typename F> static void by_ends(int64_t cols, bool in_place, F&& launch)
+{
+    if (cols % 8 == 0) launch(std::integral_constant<RowEnds, ROWS_WHOLE>());
+    else if (cols > 8 && !in_place) launch(std::integral_constant<RowEnds, ROWS_RAGGED>());
+    else launch(std::integral_constant<RowEnds, ROWS_OWN>());
+}
 template <int U> static unsigned ckpt_grid(const Chunks& c) { return (unsigned)((c.total + CK_THREADS * U - 1) / (CK_THREADS * U)); }
 
 template <typename T> static hipError_t store_of(const void* x, int64_t ldx, int64_t rows, int64_t cols, const CkptRound& r, int8_t* q, uint8_t* e, hipStream_t s)
@@ -218,7 +236,7 @@ template <typename T> static hipError_t store_of(const void* x, int64_t ldx, int
     a.in = (const T*)x;
     a.ld_in = ldx;
     a.r = r;
-    k_ckpt_store<T, 2><<<ckpt_grid<2>(a.c), CK_THREADS, 0, s>>>(a);
+    by_ends(cols, false, [&](auto ends) { k_ckpt_store<T, decltype(ends)::value, 2><<<ckpt_grid<2>(a.c), CK_THREADS, 0, s>>>(a); });
     return hipGetLastError();
 }
 hipError_t launch_ckpt_store(const void* x, int32_t dtype, int64_t ldx, int64_t rows, int64_t cols, int32_t round_mode, uint64_t seed,
@@ -259,12 +277,15 @@ static hipError_t act_backward_of(const int8_t* q, const uint8_t* e, int64_t row
     a.ld_out = lddx;
     a.coeff = coeff;
     const unsigned grid = ckpt_grid<2>(a.c);
-    switch (act) {
-        case FF_ACT_RELU: k_ckpt_act_backward<T, FF_ACT_RELU, 2><<<grid, CK_THREADS, 0, s>>>(a); break;
-        case FF_ACT_GELU: k_ckpt_act_backward<T, FF_ACT_GELU, 2><<<grid, CK_THREADS, 0, s>>>(a); break;
-        case FF_ACT_SILU: k_ckpt_act_backward<T, FF_ACT_SILU, 2><<<grid, CK_THREADS, 0, s>>>(a); break;
-        default: k_ckpt_act_backward<T, FF_ACT_IDENTITY, 2><<<grid, CK_THREADS, 0, s>>>(a); break;
-    }
+    by_ends(cols, dy == dx, [&](auto ends) {
+        constexpr RowEnds E = decltype(ends)::value;
+        switch (act) {
+            case FF_ACT_RELU: k_ckpt_act_backward<T, FF_ACT_RELU, E, 2><<<grid, CK_THREADS, 0, s>>>(a); break;
+            case FF_ACT_GELU: k_ckpt_act_backward<T, FF_ACT_GELU, E, 2><<<grid, CK_THREADS, 0, s>>>(a); break;
+            case FF_ACT_SILU: k_ckpt_act_backward<T, FF_ACT_SILU, E, 2><<<grid, CK_THREADS, 0, s>>>(a); break;
+            default: k_ckpt_act_backward<T, FF_ACT_IDENTITY, E, 2><<<grid, CK_THREADS, 0, s>>>(a); break;
+        }
+    });
     return hipGetLastError();
 }
 hipError_t launch_ckpt_act_backward(const int8_t* q, const uint8_t* e, int64_t rows, int64_t cols, int32_t act, const float* coeff,

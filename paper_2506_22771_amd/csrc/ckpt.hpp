@@ -167,6 +167,54 @@ __device__ __forceinline__ void opaque(uint32_t& v) { asm volatile("" : "+v"(v))
 __device__ __forceinline__ void opaque_uniform(int& v) { asm volatile("" : "+s"(v)); }
 __device__ __forceinline__ void opaque(float& v) { asm volatile("" : "+v"(v)); }
 
+// ---- a row's chunks -----------------------------------------------------------------------------------------------------
+// Where rows end: with a chunk; inside one, with at least eight columns; anywhere; anywhere, and no column but the chunk's own is read, because other
+// lanes may write theirs first.
+enum RowEnds { ROWS_WHOLE, ROWS_RAGGED, ROWS_ANY, ROWS_OWN };
+// Chunk c, n of whose columns exist (none: n <= 0), without a branch, behind which the compiler would count on fewer loads under way than there are.
+// What is not there is read from the row's first chunk, and the chunk that a row ends in as the row's last eight columns; `settle` makes zeros of what does
+// not exist when the values are needed.
+template <RowEnds ENDS, typename T> __device__ __forceinline__ Raw8<T> row_chunk(const T* row, int c, int n, int cols)
+{
+    if (ENDS == ROWS_OWN || (ENDS == ROWS_ANY && cols < 8)) return load_raw(row + 8 * c, max(0, n));
+    return load_raw(row + (n <= 0 ? 0 : ENDS != ROWS_WHOLE && n < 8 ? cols - 8 : 8 * c), 8);
+}
+template <int WORD> __device__ __forceinline__ void move_down(uint32_t (&w)[8 / WORD], int by)   // by: elements, 1 .. 8; WORD: elements of a word
+{
+    constexpr int W = 8 / WORD;
+#pragma unroll
+    for (int step = 4; step >= WORD; step /= 2)
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[i] = by & step ? (i + step / WORD < W ? w[i + step / WORD] : 0u) : w[i];
+    if constexpr (WORD == 2)
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[i] = by & 1 ? __builtin_amdgcn_alignbit(i + 1 < W ? w[i + 1] : 0u, w[i], 16) : w[i];
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[i] = by & 8 ? 0u : w[i];
+}
+template <RowEnds ENDS, typename T> __device__ __forceinline__ void settle(Raw8<T>& r, int n, int cols)
+{
+    if (n >= 8 || ENDS == ROWS_OWN || (ENDS == ROWS_ANY && cols < 8)) return;
+    constexpr int W = sizeof(T) == 4 ? 8 : 4;
+    uint32_t w[W];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        w[i] = r.a[i];
+        if constexpr (W == 8) w[4 + i] = r.b[i];
+    }
+    if constexpr (ENDS != ROWS_WHOLE) {
+        move_down<8 / W>(w, 8 - max(0, n));
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i) w[i] = 0;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r.a[i] = w[i];
+        if constexpr (W == 8) r.b[i] = w[4 + i];
+    }
+}
+
 // ---- a block's exponent byte and the codes of a chunk -------------------------------------------------------------------
 // A chunk is a lane's eight columns; the four lanes of a quad hold a block.
 __device__ __forceinline__ uint32_t quad_max_u32(uint32_t v)

@@ -88,49 +88,7 @@ template <typename T> __device__ __forceinline__ void load_param(const void* p, 
     }
 }
 
-// A row's chunk c, n of whose `cols` columns exist, without a branch, behind which the compiler would count on fewer loads under way than there are.
-// A chunk is there or is not, and what is not is read from the row's first one.  RAGGED: rows end inside a chunk; that one is read as the row's last
-// eight columns.  `settle` makes zeros of what does not exist, when the values are needed.
-template <bool RAGGED, int LANES, typename T> __device__ __forceinline__ Raw8<T> row_chunk(const T* row, int c, int n, int cols)
-{
-    if (RAGGED && LANES == 4 && cols < 8) return load_raw(row, n);
-    return load_raw(row + (n <= 0 ? 0 : RAGGED && n < 8 ? cols - 8 : 8 * c), 8);
-}
-template <int WORD> __device__ __forceinline__ void move_down(uint32_t (&w)[8 / WORD], int by)   // by: elements, 1 .. 8
-{
-    constexpr int W = 8 / WORD;   // WORD: elements of a word
-#pragma unroll
-    for (int step = 4; step >= WORD; step /= 2)
-#pragma unroll
-        for (int i = 0; i < W; ++i) w[i] = by & step ? (i + step / WORD < W ? w[i + step / WORD] : 0u) : w[i];
-    if constexpr (WORD == 2)
-#pragma unroll
-        for (int i = 0; i < W; ++i) w[i] = by & 1 ? __builtin_amdgcn_alignbit(i + 1 < W ? w[i + 1] : 0u, w[i], 16) : w[i];
-#pragma unroll
-    for (int i = 0; i < W; ++i) w[i] = by & 8 ? 0u : w[i];
-}
-template <bool RAGGED, int LANES, typename T> __device__ __forceinline__ void settle(Raw8<T>& r, int n, int cols)
-{
-    if (n >= 8 || (RAGGED && LANES == 4 && cols < 8)) return;
-    constexpr int W = sizeof(T) == 4 ? 8 : 4;
-    uint32_t w[W];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        w[i] = r.a[i];
-        if constexpr (W == 8) w[4 + i] = r.b[i];
-    }
-    if constexpr (RAGGED) {
-        move_down<8 / W>(w, 8 - n);
-    } else {
-#pragma unroll
-        for (int i = 0; i < W; ++i) w[i] = 0;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        r.a[i] = w[i];
-        if constexpr (W == 8) r.b[i] = w[4 + i];
-    }
-}
+template <int LANES> constexpr RowEnds row_ends(bool ragged) { return !ragged ? ROWS_WHOLE : LANES == 4 ? ROWS_ANY : ROWS_RAGGED; }
 template <bool RAGGED, typename T> __device__ __forceinline__ void row_store(T* row, int c, int n, const float v[8])
 {
     if constexpr (RAGGED) store8(row + 8 * c, n, v);
@@ -173,7 +131,7 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForw
     auto fetch = [&](int64_t row) {
         const T* const x = a.x + row * a.ldx;
 #pragma unroll
-        for (int i = 0; i < CH; ++i) raw[i] = row_chunk<RAGGED, LANES>(x, j + i * LANES, count(i), cols);
+        for (int i = 0; i < CH; ++i) raw[i] = row_chunk<row_ends<LANES>(RAGGED)>(x, j + i * LANES, count(i), cols);
     };
     int64_t row = there ? row0 : a.rows - 1;
     fetch(row);
@@ -190,7 +148,7 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForw
         float v[CH][8], sum[1] = {0};
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            settle<RAGGED, LANES>(raw[i], count(i), cols);
+            settle<row_ends<LANES>(RAGGED)>(raw[i], count(i), cols);
             raw_values(raw[i], v[i]);
 #pragma unroll
             for (int u = 0; u < 8; ++u) sum[0] += v[i][u];
@@ -384,10 +342,10 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_backward(NormBac
                     to.x[k][i] = n > 0 ? q : u32x2{0, 0};
                     to.e[k][i] = n > 0 ? e : 127u;
                 } else {
-                    to.x[k][i] = row_chunk<RAGGED, LANES>(a.x + row * a.ldx, c, n, cols);
+                    to.x[k][i] = row_chunk<row_ends<LANES>(RAGGED)>(a.x + row * a.ldx, c, n, cols);
                     to.e[k][i] = 0;
                 }
-                to.d[k][i] = row_chunk<RAGGED, LANES>(a.dy + row * a.lddy, c, n, cols);
+                to.d[k][i] = row_chunk<row_ends<LANES>(RAGGED)>(a.dy + row * a.lddy, c, n, cols);
             }
             const float rstd = a.rstd[row], mean = KEPT ? 0.0f : a.mean[row];
             to.rstd[k] = there ? rstd : 0.0f;
@@ -426,8 +384,8 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_backward(NormBac
                 // (a column that does not exist has d = 0 and adds nothing, or a NaN where the row's own columns have them too)
                 float d[8], h[8], w[8];
                 const int n = row_of(it, k) < a.rows ? count(i) : 0;
-                settle<RAGGED, LANES>(now.d[k][i], n, cols);
-                if constexpr (!KEPT) settle<RAGGED, LANES>(now.x[k][i], n, cols);
+                settle<row_ends<LANES>(RAGGED)>(now.d[k][i], n, cols);
+                if constexpr (!KEPT) settle<row_ends<LANES>(RAGGED)>(now.x[k][i], n, cols);
                 values(now, k, i, d, h);
                 weight(i, w);
 #pragma unroll

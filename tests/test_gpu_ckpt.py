@@ -216,3 +216,21 @@ def test_work_on_another_stream():
         ff.ff_ckpt_load(q, e, back)
     side.synchronize()
     assert (back == 20).all()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("rows, cols", [(3000, 101), (999, 13), (2000, 3), (40, 4097)])
+def test_activation_gradient_in_place_of_many_ragged_rows(rows, cols, dtype):
+    """Rows end inside chunks that other wavefronts share with their neighbours: none may read what another has written."""
+    g = torch.Generator("cuda").manual_seed(rows)
+    q, e = ff.ckpt_empty(rows, cols)
+    ff.ff_ckpt_store(torch.randn((rows, cols), device="cuda", generator=g), ff.ROUND_NEAREST, 0, 0, q, e)
+    c = torch.randn(rows, device="cuda", generator=g)
+    dy = torch.randn((rows, cols), device="cuda", generator=g).to(DTYPES[dtype])
+    for kind in ("gelu", "identity"):
+        for coeff in (c, None):
+            dx = torch.empty_like(dy)
+            ff.ff_ckpt_act_backward(q, e, ACTS[kind], coeff, dy, dx)
+            over = dy.clone()
+            ff.ff_ckpt_act_backward(q, e, ACTS[kind], coeff, over, over)
+            assert torch.equal(over, dx)
