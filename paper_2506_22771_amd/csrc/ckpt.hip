@@ -27,14 +27,18 @@ static Chunks chunks_of(int64_t rows, int64_t bytes_or_cols)
     const int64_t slots = (bytes_or_cols + 31) / 32 * 4;
     return {rows * slots, (uint32_t)slots, (uint32_t)(((uint64_t(1) << 32) + (uint64_t)slots - 1) / (uint64_t)slots)};
 }
-// Row and chunk of `at` chunks (fewer than 4096) behind the workgroup's first one, (row0, chunk0).  Rows of 4096 chunks or more: at most one row
-// further; shorter ones: at + chunk0 < 8192, where the product with the rounded-up reciprocal has the quotient exactly.
-__device__ __forceinline__ void chunk_place(const Chunks& c, int64_t row0, uint32_t chunk0, uint32_t at, int64_t& row, uint32_t& chunk)
+// Row (from the workgroup's first one, row0, on) and chunk of `at` chunks (fewer than 4096) behind the workgroup's first one, (row0, chunk0).  Rows of 4096
+// chunks or more: at most one row further; shorter ones: at + chunk0 < 8192, where the product with the rounded-up reciprocal has the quotient exactly.
+__device__ __forceinline__ void chunk_place(const Chunks& c, uint32_t chunk0, uint32_t at, uint32_t& r, uint32_t& chunk)
 {
     const uint32_t o = chunk0 + at;
-    const uint32_t r = c.slots >= 4096u ? (o >= c.slots ? 1u : 0u) : __umulhi(o, c.magic);
-    row = row0 + r;
+    r = c.slots >= 4096u ? (o >= c.slots ? 1u : 0u) : __umulhi(o, c.magic);
     chunk = o - r * c.slots;
+}
+// Element `at` of row row0 + r: the workgroup's part is scalar, a lane's one product of 32 by 32 bits (rows are at most 2^31 elements apart).
+template <typename T> __device__ __forceinline__ T* element(T* p, int64_t ld, int64_t row0, uint32_t r, uint32_t at)
+{
+    return p + row0 * ld + ((uint64_t)r * (uint32_t)ld + at);
 }
 __device__ __forceinline__ void chunk_first(const Chunks& c, int64_t first, int64_t& row0, uint32_t& chunk0)
 {
@@ -59,12 +63,13 @@ template <typename T> struct CkptArgs {
     int32_t cols, act;
 };
 
-// A chunk `at` chunks behind the workgroup's first one: its place (that of the matrix' first where there is none) and how many of its columns exist.
-__device__ __forceinline__ int chunk_at(const Chunks& c, int cols, int64_t first, int64_t row0, uint32_t chunk0, uint32_t at, int64_t& row, uint32_t& chunk)
+// A chunk `at` chunks behind the workgroup's first one: its place (the workgroup's first row's first chunk where there is none) and how many of its columns
+// exist.
+__device__ __forceinline__ int chunk_at(const Chunks& c, int cols, int64_t first, uint32_t chunk0, uint32_t at, uint32_t& r, uint32_t& chunk)
 {
-    chunk_place(c, row0, chunk0, at, row, chunk);
+    chunk_place(c, chunk0, at, r, chunk);
     const bool there = first + at < c.total;
-    row = there ? row : 0;
+    r = there ? r : 0;
     chunk = there ? chunk : 0;
     return there ? max(0, min(8, cols - 8 * (int)chunk)) : 0;
 }
@@ -76,13 +81,12 @@ template <typename T, RowEnds ENDS, int U> __global__ __launch_bounds__(CK_THREA
     uint32_t chunk0;
     chunk_first(a.c, first, row0, chunk0);
     Raw8<T> raw[U];
-    int64_t row[U];
-    uint32_t chunk[U];
+    uint32_t r[U], chunk[U];
     int n[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-        n[i] = chunk_at(a.c, a.cols, first, row0, chunk0, i * CK_THREADS + threadIdx.x, row[i], chunk[i]);
-        raw[i] = row_chunk<ENDS>(a.in + row[i] * a.ld_in, (int)chunk[i], n[i], a.cols);
+        n[i] = chunk_at(a.c, a.cols, first, chunk0, i * CK_THREADS + threadIdx.x, r[i], chunk[i]);
+        raw[i] = row_chunk<ENDS>(element(a.in, a.ld_in, row0, r[i], 0), (int)chunk[i], n[i], a.cols);
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
@@ -90,8 +94,10 @@ template <typename T, RowEnds ENDS, int U> __global__ __launch_bounds__(CK_THREA
         settle<ENDS>(raw[i], n[i], a.cols);
         raw_values(raw[i], v);
         const uint32_t m = quad_max_u32(abs_max_bits(v)), e = ckpt_exponent(m);
-        const u32x2 q = ckpt_codes(v, m, e, a.r, (uint64_t)row[i] * (uint64_t)a.cols + 8 * (uint64_t)chunk[i]);
-        if (first + i * CK_THREADS + threadIdx.x < a.c.total) ckpt_store_chunk(a.k, row[i], (int)chunk[i], (int)a.c.slots, n[i] > 0, q, e);
+        const u32x2 q = ckpt_codes(v, m, e, a.r, (uint64_t)row0 * (uint64_t)a.cols + ((uint64_t)r[i] * (uint32_t)a.cols + 8 * chunk[i]));
+        if (first + i * CK_THREADS + threadIdx.x < a.c.total)
+            ckpt_store_chunk(a.k, element(a.k.q, a.k.pitch, row0, r[i], 0), element(a.k.e, a.k.epitch, row0, r[i], 0), (int)chunk[i], (int)a.c.slots,
+                             n[i] > 0, q, e);
     }
 }
 
@@ -112,17 +118,14 @@ template <typename T, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckp
     int n[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-        const uint32_t at = i * CK_THREADS + threadIdx.x;
-        int64_t row;
-        uint32_t chunk;
-        chunk_place(a.c, row0, chunk0, at, row, chunk);
-        n[i] = first + at < a.c.total ? min(8, a.cols - 8 * (int)chunk) : 0;
-        to[i] = a.out + row * a.ld_out + 8 * chunk;
+        uint32_t r, chunk;
+        n[i] = chunk_at(a.c, a.cols, first, chunk0, i * CK_THREADS + threadIdx.x, r, chunk);
+        to[i] = element(a.out, a.ld_out, row0, r, 8 * chunk);
         q[i] = u32x2{0, 0};
         e[i] = 127;
         if (n[i] > 0) {
-            q[i] = *(const u32x2*)(a.k.q + row * a.k.pitch + 8 * chunk);
-            e[i] = a.k.e[row * a.k.epitch + (chunk >> 2)];
+            q[i] = *(const u32x2*)element(a.k.q, a.k.pitch, row0, r, 8 * chunk);
+            e[i] = *element(a.k.e, a.k.epitch, row0, r, chunk >> 2);
         }
     }
 #pragma unroll
@@ -137,7 +140,7 @@ template <typename T, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckp
 
 // f(u) and f'(u).  GELU: Phi(-|u|) = 1/2 t (a1 + t (a2 + ...)) exp(-u^2/2), t = 1 / (1 + p |u| / sqrt 2): Abramowitz and Stegun 7.1.26, off by at
 // most 0.75e-7 (about one unit of fp32 at 1), and its exponential is the density's too.  The large case below is bound by vector arithmetic before it is bound by
-// memory: 16384 x 4096 bf16 values 96 us with the library's erf and exp, 65 this way (75 with loads behind branches and six operations a value more).
+// memory: 16384 x 4096 bf16 values 96 us with the library's erf and exp, 65 this way (75 with loads behind branches and more of it).
 template <int ACT> __device__ __forceinline__ void act_of(float u, float& f, float& d)
 {
     if constexpr (ACT == FF_ACT_RELU) {
@@ -183,15 +186,14 @@ template <typename T, int ACT, RowEnds ENDS, int U> __global__ __launch_bounds__
     int n[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-        int64_t row;
-        uint32_t chunk;
-        n[i] = chunk_at(a.c, a.cols, first, row0, chunk0, i * CK_THREADS + threadIdx.x, row, chunk);
-        to[i] = a.out + row * a.ld_out + 8 * chunk;
-        raw[i] = row_chunk<ENDS>(in + row * ld_in, (int)chunk, a.in ? n[i] : 0, a.cols);
+        uint32_t r, chunk;
+        n[i] = chunk_at(a.c, a.cols, first, chunk0, i * CK_THREADS + threadIdx.x, r, chunk);
+        to[i] = element(a.out, a.ld_out, row0, r, 8 * chunk);
+        raw[i] = row_chunk<ENDS>(element(in, ld_in, row0, r, 0), (int)chunk, a.in ? n[i] : 0, a.cols);
         chunk = n[i] > 0 ? chunk : 0;   // (the row's pitch ends before its last block)
-        q[i] = *(const u32x2*)(a.k.q + row * a.k.pitch + 8 * chunk);
-        e[i] = a.k.e[row * a.k.epitch + (chunk >> 2)];
-        c[i] = coeff[row * ld_c];
+        q[i] = *(const u32x2*)element(a.k.q, a.k.pitch, row0, r, 8 * chunk);
+        e[i] = *element(a.k.e, a.k.epitch, row0, r, chunk >> 2);
+        c[i] = *element(coeff, ld_c, row0, r, 0);
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {

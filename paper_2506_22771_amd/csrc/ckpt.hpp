@@ -309,14 +309,14 @@ static inline CkptPtr ckpt_ptr(const void* q, const void* e, int64_t cols)
     const int64_t nb = ckpt_blocks(cols);
     return {(int8_t*)q, (uint8_t*)e, pitch8(cols), pitch8(nb), (int32_t)nb};
 }
-// Lane `j` of a row's `slots` lanes (a multiple of four that covers the row's pitch) stores its chunk's codes, its block's exponent and its share of
-// the pad bytes, which are zero.  `live`: the lane's chunk holds columns.
-__device__ __forceinline__ void ckpt_store_chunk(const CkptPtr& k, int64_t row, int chunk, int slots, bool live, u32x2 q, uint32_t e)
+// Lane `chunk` of a row's `slots` lanes (a multiple of four that covers the row's pitch) stores its chunk's codes, its block's exponent and its share of
+// the pad bytes, which are zero.  `live`: the lane's chunk holds columns; q_row, e_row: where the row begins.
+__device__ __forceinline__ void ckpt_store_chunk(const CkptPtr& k, int8_t* q_row, uint8_t* e_row, int chunk, int slots, bool live, u32x2 q, uint32_t e)
 {
-    if ((int64_t)chunk * 8 < k.pitch) *(u32x2*)(k.q + row * k.pitch + (int64_t)chunk * 8) = live ? q : u32x2{0, 0};
+    if ((int64_t)chunk * 8 < k.pitch) *(u32x2*)(q_row + (uint32_t)chunk * 8) = live ? q : u32x2{0, 0};
     const int b = chunk >> 2;
-    if ((chunk & 3) == 0 && b < k.blocks) k.e[row * k.epitch + b] = (uint8_t)e;
-    for (int p = k.blocks + chunk; p < (int)k.epitch; p += slots) k.e[row * k.epitch + p] = 0;
+    if ((chunk & 3) == 0 && b < k.blocks) e_row[b] = (uint8_t)e;
+    for (int p = k.blocks + chunk; p < (int)k.epitch; p += slots) e_row[p] = 0;
 }
 
 }  // namespace ffi

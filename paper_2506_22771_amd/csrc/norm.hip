@@ -192,7 +192,7 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForw
             if (a.k.q) {
                 const uint32_t m = quad_max_u32(abs_max_bits(h)), e = ckpt_exponent(m);
                 const u32x2 q = ckpt_codes(h, m, e, a.r, (uint64_t)row * (uint64_t)a.cols + 8 * (uint64_t)c);
-                if (there) ckpt_store_chunk(a.k, row, c, LANES * CH, n > 0, q, e);
+                if (there) ckpt_store_chunk(a.k, a.k.q + row * a.k.pitch, a.k.e + row * a.k.epitch, c, LANES * CH, n > 0, q, e);
             }
         }
         if (!MANY || next >= a.rows) break;
@@ -251,7 +251,7 @@ template <typename T> __global__ __launch_bounds__(1024) void k_norm_forward_wid
         if (a.k.q) {
             const uint32_t m = quad_max_u32(abs_max_bits(h)), e = ckpt_exponent(m);
             const u32x2 q = ckpt_codes(h, m, e, a.r, (uint64_t)row * (uint64_t)a.cols + 8 * (uint64_t)c);
-            ckpt_store_chunk(a.k, row, c, chunks, n > 0, q, e);
+            ckpt_store_chunk(a.k, a.k.q + row * a.k.pitch, a.k.e + row * a.k.epitch, c, chunks, n > 0, q, e);
         }
     }
 }
