@@ -35,11 +35,6 @@ __device__ __forceinline__ void chunk_place(const Chunks& c, uint32_t chunk0, ui
     r = c.slots >= 4096u ? (o >= c.slots ? 1u : 0u) : __umulhi(o, c.magic);
     chunk = o - r * c.slots;
 }
-// Element `at` of row row0 + r: the workgroup's part is scalar, a lane's one product of 32 by 32 bits (rows are at most 2^31 elements apart).
-template <typename T> __device__ __forceinline__ T* element(T* p, int64_t ld, int64_t row0, uint32_t r, uint32_t at)
-{
-    return p + row0 * ld + ((uint64_t)r * (uint32_t)ld + at);
-}
 __device__ __forceinline__ void chunk_first(const Chunks& c, int64_t first, int64_t& row0, uint32_t& chunk0)
 {
     if (first >> 32) {

@@ -167,6 +167,12 @@ __device__ __forceinline__ void opaque(uint32_t& v) { asm volatile("" : "+v"(v))
 __device__ __forceinline__ void opaque_uniform(int& v) { asm volatile("" : "+s"(v)); }
 __device__ __forceinline__ void opaque(float& v) { asm volatile("" : "+v"(v)); }
 
+// Element `at` of row row0 + r: row0, the workgroup's part, is scalar, a lane's is one product of 32 by 32 bits (rows are at most 2^31 elements apart).
+template <typename T> __device__ __forceinline__ T* element(T* p, int64_t ld, int64_t row0, uint32_t r, uint32_t at)
+{
+    return p + row0 * ld + ((uint64_t)r * (uint32_t)ld + at);
+}
+
 // ---- a row's chunks -----------------------------------------------------------------------------------------------------
 // Where rows end: with a chunk; inside one, with at least eight columns; anywhere; anywhere, and no column but the chunk's own is read, because other
 // lanes may write theirs first.

@@ -122,18 +122,20 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForw
     constexpr bool MANY = many_rows(LANES, CH);
     __shared__ float red[2][W];   // (a sum's words are written again behind the other sum's barrier)
     const int j = threadIdx.x % LANES;
-    const int64_t row0 = (int64_t)blockIdx.x * Group<LANES>::ROWS + Group<LANES>::mine();
+    const int64_t first = (int64_t)blockIdx.x * Group<LANES>::ROWS;   // the workgroup's; `row` is that, or the wavefront's, and r the group's row behind it
+    const int64_t row0 = first + Group<LANES>::mine();
     if (LANES == 64 && row0 >= a.rows) return;   // (a whole wavefront, which meets no other)
     const bool there = Group<LANES>::ROWS == 1 || LANES == 64 || row0 < a.rows;   // (lanes of a row that does not exist go along and store nothing)
     int cols = a.cols;
     auto count = [&](int i) { return max(0, min(8, cols - 8 * (j + i * LANES))); };
     Raw8<T> raw[CH];
+    int64_t row = LANES < 64 ? first : row0;
+    const uint32_t r = LANES < 64 && there ? Group<LANES>::mine() : 0;
     auto fetch = [&](int64_t row) {
-        const T* const x = a.x + row * a.ldx;
+        const T* const x = element(a.x, a.ldx, row, r, 0);
 #pragma unroll
         for (int i = 0; i < CH; ++i) raw[i] = row_chunk<row_ends<LANES>(RAGGED)>(x, j + i * LANES, count(i), cols);
     };
-    int64_t row = there ? row0 : a.rows - 1;
     fetch(row);
     float w[MANY ? CH : 1][8], b[MANY ? CH : 1][8];
     auto params = [&](int i, float* w, float* b) {
@@ -174,10 +176,10 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForw
         group_sum<LANES, 1>(sum, red[1]);
         const float rstd = inverse_root(sum[0] * a.inv_cols + a.eps);
         if (there && j == 0) {
-            if (a.mean) a.mean[row] = mean;
-            if (a.rstd) a.rstd[row] = rstd;
+            if (a.mean) a.mean[row + r] = mean;
+            if (a.rstd) a.rstd[row + r] = rstd;
         }
-        T* const y = a.y + row * a.ldy;
+        T* const y = element(a.y, a.ldy, row, r, 0);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             opaque_uniform(cols);
@@ -191,8 +193,9 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForw
             row_store<RAGGED>(y, c, there ? n : 0, o);
             if (a.k.q) {
                 const uint32_t m = quad_max_u32(abs_max_bits(h)), e = ckpt_exponent(m);
-                const u32x2 q = ckpt_codes(h, m, e, a.r, (uint64_t)row * (uint64_t)a.cols + 8 * (uint64_t)c);
-                if (there) ckpt_store_chunk(a.k, a.k.q + row * a.k.pitch, a.k.e + row * a.k.epitch, c, LANES * CH, n > 0, q, e);
+                const u32x2 q = ckpt_codes(h, m, e, a.r, (uint64_t)row * (uint64_t)a.cols + ((uint64_t)r * (uint32_t)a.cols + 8 * (uint32_t)c));
+                if (there)
+                    ckpt_store_chunk(a.k, element(a.k.q, a.k.pitch, row, r, 0), element(a.k.e, a.k.epitch, row, r, 0), c, LANES * CH, n > 0, q, e);
             }
         }
         if (!MANY || next >= a.rows) break;
@@ -325,29 +328,32 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_backward(NormBac
         uint32_t e[R][CH];
         float mean[R], rstd[R];
     };
-    // Row k of round `it`; one that does not exist is the last row, with zeros for everything.
-    auto row_of = [&](int64_t it, int k) { return (it * R + k) * groups + g0; };
+    // Row k of round `it`, as a scalar and what a lane's group adds to it; one that does not exist is some other, with zeros for everything.
+    const uint32_t own = LANES < 64 ? group : 0;
+    const int64_t base = LANES < 64 ? (int64_t)blockIdx.x * G::ROWS : g0;
+    auto row_of = [&](int64_t it, int k) { return (it * R + k) * groups + base; };
     auto fetch = [&](int64_t it, Rows& to) {
 #pragma unroll
         for (int k = 0; k < R; ++k) {
-            const bool there = row_of(it, k) < a.rows;
-            const int64_t row = there ? row_of(it, k) : a.rows - 1;
+            const bool there = row_of(it, k) + own < a.rows;
+            const int64_t row = min(row_of(it, k), a.rows - 1);
+            const uint32_t r = there ? own : 0;
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
                 const int c = j + i * LANES, n = there ? count(i) : 0;
                 if constexpr (KEPT) {
                     const int at = n > 0 ? c : 0;
-                    const u32x2 q = *(const u32x2*)(a.k.q + row * a.k.pitch + 8 * at);
-                    const uint32_t e = a.k.e[row * a.k.epitch + (at >> 2)];
+                    const u32x2 q = *(const u32x2*)element(a.k.q, a.k.pitch, row, r, 8 * at);
+                    const uint32_t e = *element(a.k.e, a.k.epitch, row, r, at >> 2);
                     to.x[k][i] = n > 0 ? q : u32x2{0, 0};
                     to.e[k][i] = n > 0 ? e : 127u;
                 } else {
-                    to.x[k][i] = row_chunk<row_ends<LANES>(RAGGED)>(a.x + row * a.ldx, c, n, cols);
+                    to.x[k][i] = row_chunk<row_ends<LANES>(RAGGED)>(element(a.x, a.ldx, row, r, 0), c, n, cols);
                     to.e[k][i] = 0;
                 }
-                to.d[k][i] = row_chunk<row_ends<LANES>(RAGGED)>(a.dy + row * a.lddy, c, n, cols);
+                to.d[k][i] = row_chunk<row_ends<LANES>(RAGGED)>(element(a.dy, a.lddy, row, r, 0), c, n, cols);
             }
-            const float rstd = a.rstd[row], mean = KEPT ? 0.0f : a.mean[row];
+            const float rstd = a.rstd[row + r], mean = KEPT ? 0.0f : a.mean[row + r];
             to.rstd[k] = there ? rstd : 0.0f;
             to.mean[k] = there ? mean : 0.0f;
         }
@@ -383,7 +389,7 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_backward(NormBac
             for (int i = 0; i < CH; ++i) {
                 // (a column that does not exist has d = 0 and adds nothing, or a NaN where the row's own columns have them too)
                 float d[8], h[8], w[8];
-                const int n = row_of(it, k) < a.rows ? count(i) : 0;
+                const int n = row_of(it, k) + own < a.rows ? count(i) : 0;
                 settle<row_ends<LANES>(RAGGED)>(now.d[k][i], n, cols);
                 if constexpr (!KEPT) settle<row_ends<LANES>(RAGGED)>(now.x[k][i], n, cols);
                 values(now, k, i, d, h);
@@ -419,7 +425,7 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_backward(NormBac
                     weight(i, w);
 #pragma unroll
                     for (int u = 0; u < 8; ++u) d[u] = now.rstd[k] * (d[u] * w[u] - c1 - h[u] * c2);
-                    row_store<RAGGED>(a.dx + row * a.lddx, j + i * LANES, row < a.rows ? count(i) : 0, d);
+                    row_store<RAGGED>(element(a.dx, a.lddx, row, own, 0), j + i * LANES, row + own < a.rows ? count(i) : 0, d);
                     if constexpr (CH == 4) __builtin_amdgcn_sched_barrier(0);
                 }
             }
