@@ -4,8 +4,8 @@
 //   act backward:  dx = (dy + 2 c[row] f(u)) f'(u), u the checkpointed argument of f; 2 c f(u) is the gradient of c G, the goodness
 //                  G = sum f(u)^2 of Section III (dL/dG = c), dy what comes down from the layers above (either may be absent)
 //
-// Measured, us and TB/s, 16384 x 4096 (a copy of as many bytes reaches 5.3): bf16 store 31 (6.5), with stochastic rounding 45-49 (4.2, by its arithmetic:
-// 25 operations a value), load 30 (6.8), GELU backward 65 (5.2); fp32 60 (5.6), 63 (5.4), 71 (4.8), 110 (5.5).
+// Measured, us and TB/s, 16384 x 4096 (a copy of as many bytes reaches 5.3): bf16 store 31 (6.5), with stochastic rounding 43-48 (4.5, by its arithmetic:
+// 25 operations a value), load 30 (6.8), GELU backward 62-65 (5.3); fp32 60 (5.6), 63 (5.4), 71 (4.8), 110 (5.5).
 // All three are bound by memory but for that.  A lane has eight columns (a chunk) of a row, a quad of lanes one block; a workgroup takes consecutive chunks,
 // whatever the row length, and has all its loads in flight before the first is used.
 #include <type_traits>
@@ -134,8 +134,8 @@ template <typename T, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckp
 }
 
 // f(u) and f'(u).  GELU: Phi(-|u|) = 1/2 t (a1 + t (a2 + ...)) exp(-u^2/2), t = 1 / (1 + p |u| / sqrt 2): Abramowitz and Stegun 7.1.26, off by at
-// most 0.75e-7 (about one unit of fp32 at 1), and its exponential is the density's too.  The large case below is bound by vector arithmetic before it is bound by
-// memory: 16384 x 4096 bf16 values 96 us with the library's erf and exp, 65 this way (75 with loads behind branches and more of it).
+// most 0.75e-7 (about one unit of fp32 at 1), and its exponential is the density's too.  With more arithmetic than this the large case is bound by it and not by
+// memory: 16384 x 4096 bf16 values 96 us with the library's erf and exp, 62 to 65 this way.
 template <int ACT> __device__ __forceinline__ void act_of(float u, float& f, float& d)
 {
     if constexpr (ACT == FF_ACT_RELU) {

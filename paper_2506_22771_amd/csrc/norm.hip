@@ -621,7 +621,8 @@ hipError_t launch_norm_forward(const NormForwardLaunch& a, hipStream_t s)
 }
 
 // Lanes of a row and workgroups of the backward pass: as many as run at once, each with a share of the rows and one set of column sums.  Up to 1024
-// columns a wavefront has a row to itself (131072 x 784 bf16: 237 us by 256 lanes with a chunk each, 144 by 64 with two); of 1025 to 2048, 256 lanes with
+// columns a wavefront has a row to itself (131072 x 784 bf16: 237 us by 256 lanes with a chunk each, 144 by 64 with two); up to 1536,
+// with three chunks, where there are many (65536 x 1100 bf16: 157 us by 256 lanes, 107 by 64; 2048 rows: 12.2 and 13.6); else up to 2048, 256 lanes with
 // one chunk (32768 x 2000 fp32: 147 us, 161 by 128 lanes with two; 2048 x 2000 bf16: 15 and 18).
 struct NormPlan {
     int lanes, ch;   // ch == 0: rows too wide for registers
@@ -631,15 +632,15 @@ static NormPlan backward_plan(int64_t rows, int64_t cols)
 {
     const int64_t chunks = (cols + 7) / 8;
     NormPlan p;
-    if (chunks <= 128) {
-        p.ch = chunks <= 64 ? 1 : 2;
+    if (chunks <= 128 || (chunks <= 192 && rows >= 8192)) {
+        p.ch = chunks <= 64 ? 1 : chunks <= 128 ? 2 : 3;
         for (p.lanes = 4; p.lanes * p.ch < chunks; p.lanes *= 2) {}
     } else {
         p.lanes = chunks <= 512 ? 256 : 512;
         p.ch = chunks <= 256 ? 1 : chunks <= 1024 ? 2 : chunks <= 2048 ? 4 : 0;
     }
     const int64_t per = p.lanes <= 64 ? 256 / p.lanes : 1;
-    const int64_t most = p.ch == 0 ? 64 : p.lanes == 512 ? 256 : p.lanes <= 64 ? 1024 : 512;   // (of 512 lanes a compute unit holds one)
+    const int64_t most = p.ch == 0 ? 64 : p.lanes == 512 ? 256 : p.lanes <= 64 && p.ch < 3 ? 1024 : 512;   // (of 512 lanes a compute unit holds one)
     const int64_t need = (rows + per - 1) / per;
     p.wgs = need < most ? need : most;
     return p;
@@ -661,7 +662,8 @@ template <typename T, bool KEPT, bool RAGGED> static void backward_as(const Norm
     else if (p.lanes == 16) k_norm_backward<T, KEPT, 16, 1, RAGGED><<<grid, 256, 0, s>>>(a);
     else if (p.lanes == 32) k_norm_backward<T, KEPT, 32, 1, RAGGED><<<grid, 256, 0, s>>>(a);
     else if (p.lanes == 64 && p.ch == 1) k_norm_backward<T, KEPT, 64, 1, RAGGED><<<grid, 256, 0, s>>>(a);
-    else if (p.lanes == 64) k_norm_backward<T, KEPT, 64, 2, RAGGED><<<grid, 256, 0, s>>>(a);
+    else if (p.lanes == 64 && p.ch == 2) k_norm_backward<T, KEPT, 64, 2, RAGGED><<<grid, 256, 0, s>>>(a);
+    else if (p.lanes == 64) k_norm_backward<T, KEPT, 64, 3, RAGGED><<<grid, 256, 0, s>>>(a);
     else if (p.ch == 1) k_norm_backward<T, KEPT, 256, 1, RAGGED><<<grid, 256, 0, s>>>(a);
     else if (p.lanes == 256) k_norm_backward<T, KEPT, 256, 2, RAGGED><<<grid, 256, 0, s>>>(a);
     else if (p.ch == 2) k_norm_backward<T, KEPT, 512, 2, RAGGED><<<grid, 512, 0, s>>>(a);

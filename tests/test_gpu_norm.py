@@ -290,7 +290,7 @@ def test_calls_in_a_graph():
 # More rows than groups run at once, so that they go row after row, at every group that does: 64 lanes (1024 workgroups of four rows), 128 (2048 workgroups) to
 # 1024 (256), and the backward pass' few workgroups; whole chunks and rows that end inside one
 LONG = [(4400, 784, "float32"), (4200, 1001, "bfloat16"), (2200, 1500, "float16"), (1200, 3001, "float32"), (600, 6002, "bfloat16"), (300, 12001, "float16"),
-        (260, 16384, "bfloat16")]
+        (260, 16384, "bfloat16"), (8200, 1030, "bfloat16"), (8200, 1041, "float32")]
 
 
 @pytest.mark.parametrize("rows, cols, dtype", LONG)
