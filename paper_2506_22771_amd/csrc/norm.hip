@@ -261,7 +261,8 @@ template <typename T> __global__ __launch_bounds__(1024) void k_norm_forward_wid
 
 // ------------------------------------------------------------------------------------------------
 // Backward.  A workgroup keeps the column sums of its rows in registers (a lane's columns never change) and leaves them in the
-// workspace; k_norm_columns adds the workgroups' sums in order, so results do not depend on timing.
+// workspace; k_norm_columns adds the workgroups' sums in order, so results do not depend on timing.  Of few rows, other workgroups of the same launch
+// make the column sums.
 // ------------------------------------------------------------------------------------------------
 template <typename T> struct NormBackwardArgs {
     const T* dy;
@@ -277,7 +278,56 @@ template <typename T> struct NormBackwardArgs {
     float* part;        // [workgroups][2][pcols]
     int64_t pcols;
     float2* row_sums;   // rows too wide for registers: both means of every row
+    int64_t row_wgs;    // workgroups that take rows; those behind them take columns, and leave dweight and dbias
+    float* dweight;
+    float* dbias;
+    int32_t accumulate;
 };
+
+// Few rows: 64 columns of all of them and their sums, while other workgroups work on dx.  What is read twice costs less than a second launch.
+// lds: sixteen words a thread.
+template <typename T, bool KEPT, int THREADS> __device__ __forceinline__ void column_sums(const NormBackwardArgs<T>& a, int64_t part, float* lds)
+{
+    constexpr int S = THREADS / 8;
+    const int lane = threadIdx.x & 7, slice = threadIdx.x >> 3, first = (int)part * 64, at = first + 8 * lane, n = max(0, min(8, a.cols - at));
+    float dw[8], db[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) dw[u] = db[u] = 0;
+    if (n > 0) {
+#pragma unroll 4
+        for (int64_t row = slice; row < a.rows; row += S) {
+            float d[8], h[8];
+            load8(a.dy + row * a.lddy + at, n, d);
+            if constexpr (KEPT) {
+                ckpt_values(*(const u32x2*)(a.k.q + row * a.k.pitch + at), a.k.e[row * a.k.epitch + (at >> 5)], h);
+            } else {
+                const float rstd = a.rstd[row], mean = a.mean[row];
+                load8(a.x + row * a.ldx + at, n, h);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) h[u] = (h[u] - mean) * rstd;
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                dw[u] = __builtin_fmaf(d[u], h[u], dw[u]);
+                db[u] += d[u];
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+        lds[threadIdx.x * 16 + u] = dw[u];
+        lds[threadIdx.x * 16 + 8 + u] = db[u];
+    }
+    __syncthreads();
+    const int col = threadIdx.x & 63;
+    float* const out = threadIdx.x < 64 ? a.dweight : a.dbias;
+    if (threadIdx.x >= 128 || first + col >= a.cols || !out) return;
+    const float* const from = lds + (col >> 3) * 16 + (threadIdx.x >> 6) * 8 + (col & 7);
+    float v = 0;
+#pragma unroll 8
+    for (int s = 0; s < S; ++s) v += from[s * 128];
+    out[first + col] = a.accumulate ? out[first + col] + v : v;
+}
 
 // Rows of a group in a round; the next round's are on their way meanwhile.
 template <typename T, int CH> constexpr int rows_ahead() { return sizeof(T) == 4 || CH > 1 ? 1 : 2; }
@@ -288,9 +338,13 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_backward(NormBac
     using G = Group<LANES>;
     constexpr int W = LANES > 64 ? LANES / 64 : 1, R = rows_ahead<T, CH>();
     __shared__ float red[2][2 * R * W];
-    __shared__ __attribute__((aligned(16))) float cols_lds[G::ROWS > 1 ? G::THREADS * 16 : 4];
+    __shared__ __attribute__((aligned(16))) float cols_lds[G::THREADS * 16];
+    if (blockIdx.x >= a.row_wgs) {
+        column_sums<T, KEPT, G::THREADS>(a, blockIdx.x - a.row_wgs, cols_lds);
+        return;
+    }
     const int j = threadIdx.x % LANES, group = G::mine();
-    const int64_t groups = (int64_t)gridDim.x * G::ROWS, g0 = (int64_t)blockIdx.x * G::ROWS + group;
+    const int64_t groups = a.row_wgs * G::ROWS, g0 = (int64_t)blockIdx.x * G::ROWS + group;
     int cols = a.cols;
     auto count = [&](int i) { return max(0, min(8, cols - 8 * (j + i * LANES))); };
     // The weight is held in registers, or, where a lane has four chunks, in LDS: in memory its loads would wait for the next rows'.
@@ -645,6 +699,14 @@ static NormPlan backward_plan(int64_t rows, int64_t cols)
     p.wgs = need < most ? need : most;
     return p;
 }
+// One launch for rows and columns, or the workgroups' sums and a launch that adds them.  bf16, us, one launch and two: 1 x 784 3.8 and 6.8, 128 x 784 3.7 and 7.1,
+// 128 x 16384 7.1 and 17.7, 256 x 500 5.8 and 7.0, 512 x 500 9.1 and 7.5, 512 x 784 5.5 and 7.6, 512 x 4096 6.3 and 16.2, 1024 x 784 8.7 and 8.6, 1024 x 4096
+// 11.8 and 17.6; fp32: 512 x 16384 32 and 34, 1024 x 16384 58 and 50.
+static bool sums_at_once(const NormPlan& p, int64_t rows, int64_t cols)
+{
+    if (p.ch == 0 || rows == 0) return false;
+    return rows <= 256 || (rows <= 512 && cols > 512) || (rows <= 1024 && cols >= 2000 && cols <= 8192);
+}
 static int64_t padded_cols(int64_t cols) { return (cols + 7) / 8 * 8; }
 size_t norm_backward_workspace(int64_t rows, int64_t cols)
 {
@@ -654,9 +716,9 @@ size_t norm_backward_workspace(int64_t rows, int64_t cols)
     return n < FF_WS_MIN_BYTES ? FF_WS_MIN_BYTES : n;
 }
 
-template <typename T, bool KEPT, bool RAGGED> static void backward_as(const NormPlan& p, const NormBackwardArgs<T>& a, hipStream_t s)
+template <typename T, bool KEPT, bool RAGGED> static void backward_as(const NormPlan& p, const NormBackwardArgs<T>& a, int64_t column_wgs, hipStream_t s)
 {
-    const dim3 grid((unsigned)p.wgs);
+    const dim3 grid((unsigned)(a.row_wgs + column_wgs));
     if (p.lanes == 4) k_norm_backward<T, KEPT, 4, 1, RAGGED><<<grid, 256, 0, s>>>(a);
     else if (p.lanes == 8) k_norm_backward<T, KEPT, 8, 1, RAGGED><<<grid, 256, 0, s>>>(a);
     else if (p.lanes == 16) k_norm_backward<T, KEPT, 16, 1, RAGGED><<<grid, 256, 0, s>>>(a);
@@ -691,14 +753,21 @@ template <typename T, bool KEPT> static hipError_t backward_of(const NormBackwar
     a.part = (float*)l.ws;
     a.pcols = padded_cols(l.cols);
     a.row_sums = (float2*)((char*)l.ws + align_up((size_t)(p.wgs * 2 * a.pcols) * sizeof(float), 256));
+    a.dweight = l.dweight;
+    a.dbias = l.dbias;
+    a.accumulate = l.accumulate;
+    const bool at_once = a.sums && sums_at_once(p, l.rows, l.cols) && l.dx != l.dy && (!l.x || l.dx != l.x);   // (in place, rows are written while columns are read)
+    const int64_t column_wgs = at_once ? (l.cols + 63) / 64 : 0;
+    a.row_wgs = at_once && !l.dx ? 0 : p.wgs;
+    if (at_once) a.sums = 0;
     if (l.rows > 0) {
         if (p.ch == 0) {
             if (a.dx) k_norm_row_sums<T, KEPT><<<dim3((unsigned)l.rows), 1024, 0, s>>>(a);
             k_norm_backward_wide<T, KEPT><<<dim3((unsigned)((a.cols + 2047) / 2048), (unsigned)p.wgs), 256, 0, s>>>(a);
         } else if (a.cols % 8 == 0) {
-            backward_as<T, KEPT, false>(p, a, s);
+            backward_as<T, KEPT, false>(p, a, column_wgs, s);
         } else {
-            backward_as<T, KEPT, true>(p, a, s);
+            backward_as<T, KEPT, true>(p, a, column_wgs, s);
         }
         const hipError_t err = hipGetLastError();
         if (err != hipSuccess) return err;

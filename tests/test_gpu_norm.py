@@ -52,7 +52,7 @@ def check_kept(q, e, h, dh, cols, stochastic):
         at = slice(32 * b, min(cols, 32 * b + 32))
         low = np.maximum(np.abs(h[:, at]) - dh[:, at], 0).max(1)
         high = (np.abs(h[:, at]) + dh[:, at]).max(1)
-        for r in range(h.shape[0]):
+        for r in range(0, h.shape[0], 1 if h.shape[0] <= 300 else 37):
             assert N.exponent_of(low[r]) <= ge[r, b] <= N.exponent_of(high[r]) or low[r] < 2.0**-100
 
 
@@ -290,7 +290,8 @@ def test_calls_in_a_graph():
 # More rows than groups run at once, so that they go row after row, at every group that does: 64 lanes (1024 workgroups of four rows), 128 (2048 workgroups) to
 # 1024 (256), and the backward pass' few workgroups; whole chunks and rows that end inside one
 LONG = [(4400, 784, "float32"), (4200, 1001, "bfloat16"), (2200, 1500, "float16"), (1200, 3001, "float32"), (600, 6002, "bfloat16"), (300, 12001, "float16"),
-        (260, 16384, "bfloat16"), (8200, 1030, "bfloat16"), (8200, 1041, "float32")]
+        (260, 16384, "bfloat16"), (8200, 1030, "bfloat16"), (8200, 1041, "float32"),
+        (1030, 6002, "float16"), (520, 12001, "bfloat16"), (520, 16384, "float32")]
 
 
 @pytest.mark.parametrize("rows, cols, dtype", LONG)
