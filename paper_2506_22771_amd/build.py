@@ -23,7 +23,7 @@ BIND = os.path.join(HERE, "_bind.so")
 SOURCES = ["elementwise.hip", "gemm_i8.hip", "gemm_few.hip", "conv.hip", "conv3.hip", "conv3_wide.hip", "wgrad3.hip", "rows.hip", "fused.hip", "api.hip",
            "norm.hip", "ckpt.hip", "ckpt_wgrad.hip", "api_norm.hip"]
 HEADERS = [os.path.join(CSRC, "ff_internal.hpp"), os.path.join(CSRC, "device_math.hpp"), os.path.join(CSRC, "codes.hpp"), os.path.join(CSRC, "window.hpp"), os.path.join(CSRC, "ckpt.hpp"),
-           os.path.join(CSRC, "norm.hpp"), os.path.join(os.path.dirname(HERE), "include", "ffint8.h")]
+           os.path.join(CSRC, "norm.hpp"), os.path.join(CSRC, "wgrad_plan.hpp"), os.path.join(os.path.dirname(HERE), "include", "ffint8.h")]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-ffp-contract=off", "-fno-fast-math",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-function", "-Wno-inline-asm"]
 

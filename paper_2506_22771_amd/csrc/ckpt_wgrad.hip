@@ -22,6 +22,7 @@
 
 #include "ckpt.hpp"
 #include "norm.hpp"
+#include "wgrad_plan.hpp"
 
 namespace ffi {
 
@@ -174,7 +175,8 @@ __global__ __launch_bounds__(128 * WK) __attribute__((amdgpu_waves_per_eu(BT == 
     const uint8_t* const ce = a.c.e + cb;
     struct Chunk { Raw8<T> d; u32x2 q; uint32_t e; };
     // Steps in order, from scalar bases and this thread's fixed offsets.  A chunk of dy may reach into the next row (n not a multiple of
-    // eight); words beyond the end of a matrix, rows that do not exist among them, fail the buffer's range check and are zero.
+    // eight); words beyond the end of a matrix, rows that do not exist among them, fail the buffer's range check and are zero.  All of an address that
+    // can pass the end is in the vector offset: the scalar offset is no part of what is compared with the size, and may be larger than it in a step of few rows.
     const uint32_t off_d = (uint32_t)(r0 * a.lddy + cn) * sizeof(T), off_q = (uint32_t)(r0 * a.c.pitch + ck), off_e = (uint32_t)(r0 * a.c.epitch) + cb;
     const int64_t step_d = S::BM * a.lddy * (int64_t)sizeof(T), step_q = S::BM * a.c.pitch, step_e = S::BM * a.c.epitch;
     const char *base_d = (const char*)a.dy + step0 * step_d, *base_q = (const char*)a.c.q + step0 * step_q, *base_e = (const char*)a.c.e + step0 * step_e;
@@ -185,12 +187,13 @@ __global__ __launch_bounds__(128 * WK) __attribute__((amdgpu_waves_per_eu(BT == 
     };
     auto fetch = [&](int i) {
         const __amdgpu_buffer_rsrc_t bd = buffer(base_d, left_d), bq = buffer(base_q, left_q), be = buffer(base_e, left_e);
-        const int at_d = (int)(i * S::ROWS * a.lddy * (int64_t)sizeof(T)), at_q = (int)(i * S::ROWS * a.c.pitch), at_e = (int)(i * S::ROWS * a.c.epitch);
+        const uint32_t at_d = off_d + (uint32_t)(i * S::ROWS * a.lddy * (int64_t)sizeof(T)), at_q = off_q + (uint32_t)(i * S::ROWS * a.c.pitch),
+                       at_e = off_e + (uint32_t)(i * S::ROWS * a.c.epitch);
         Chunk c;
-        c.d.a = __builtin_amdgcn_raw_buffer_load_b128(bd, (int)off_d, at_d, 0);
-        if constexpr (sizeof(T) == 4) c.d.b = __builtin_amdgcn_raw_buffer_load_b128(bd, (int)off_d, at_d + 16, 0);
-        c.q = __builtin_amdgcn_raw_buffer_load_b64(bq, (int)off_q, at_q, 0);
-        c.e = __builtin_amdgcn_raw_buffer_load_b8(be, (int)off_e, at_e, 0);
+        c.d.a = __builtin_amdgcn_raw_buffer_load_b128(bd, (int)at_d, 0, 0);
+        if constexpr (sizeof(T) == 4) c.d.b = __builtin_amdgcn_raw_buffer_load_b128(bd, (int)(at_d + 16), 0, 0);
+        c.q = __builtin_amdgcn_raw_buffer_load_b64(bq, (int)at_q, 0, 0);
+        c.e = __builtin_amdgcn_raw_buffer_load_b8(be, (int)at_e, 0, 0);
         return c;
     };
     auto advance = [&](bool more) {   // to the next step, or not beyond the last (which is then fetched again and used by nobody)
@@ -437,43 +440,6 @@ __global__ __launch_bounds__(256) void k_ckpt_wgrad_sum(WgradArgs a)
 // ------------------------------------------------------------------------------------------------
 // launches
 // ------------------------------------------------------------------------------------------------
-struct WgradPlan {
-    int tile, splits;
-    int64_t steps, per;
-};
-static int plan_rows(int terms, int tile) { return terms == 3 && tile > 64 ? 16 : 32; }
-// Tile and split of the rows: the pair that takes the least time by what was measured.  Sixteen rows take a workgroup `alone` microseconds where it
-// has the compute unit to itself, and `shared` for every workgroup of the unit where there are several, up to `units` of them at once; one round of them has 2 us
-// of first loads and last stores, a sum of splits 3 us and its traffic at 5 TB/s.  (2048 rows, 2000 x 2000, fp32: 256x256 in four splits 71 us by this and 74
-// measured, 128x128 in two 76 and 81, in one 92 and 94; bf16: 41 and 46, 39 and 44, 39 and 42.)
-static WgradPlan wgrad_plan(int64_t rows, int64_t n, int64_t k, int terms)
-{
-    struct Speed { int tile, units; double alone, shared; };   // per number of terms
-    static constexpr Speed speeds[3][3] = {{{256, 1, 0.49, 0.49}, {128, 2, 0.26, 0.165}, {64, 5, 0.10, 0.075}},
-                                           {{256, 1, 0.93, 0.93}, {128, 2, 0.45, 0.30}, {64, 4, 0.17, 0.115}},
-                                           {{256, 1, 1.45, 1.45}, {128, 2, 0.67, 0.445}, {64, 3, 0.245, 0.175}}};
-    static constexpr int splits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256};
-    WgradPlan best = {64, 1, 0, 0};
-    double least = 0;
-    for (const Speed& v : speeds[terms - 1]) {
-        const int bm = plan_rows(terms, v.tile);
-        const int64_t count = ((n + v.tile - 1) / v.tile) * ((k + v.tile - 1) / v.tile), steps = (rows + bm - 1) / bm;
-        for (int s : splits) {
-            if (s > 1 && (s > steps || s * n * k > (int64_t(1) << 26))) break;
-            const int64_t per = (steps + s - 1) / s, real = per > 0 ? (steps + per - 1) / per : 1;
-            const int64_t each = (count * real + 255) / 256, rounds = (each + v.units - 1) / v.units;   // workgroups of a compute unit
-            const double alone = (double)rounds * v.alone, shared = (double)each * v.shared;
-            const double t = (double)(per * (bm / 16)) * (alone > shared ? alone : shared) + 2.0 * (double)rounds +
-                             (real > 1 ? 3.0 + (double)((real + 1) * n * k) * 4e-6 / 5.0 : 0.0);
-            if (least == 0 || t < least) {
-                least = t;
-                best = {v.tile, (int)real, steps, per};
-            }
-            if (count * s >= 2048) break;   // (every compute unit has its share)
-        }
-    }
-    return best;
-}
 static int64_t part_stride(int64_t n, int64_t k) { return (n * k + n + 3) & ~int64_t(3); }
 size_t ckpt_wgrad_workspace(int64_t rows, int64_t n, int64_t k)
 {
