@@ -3,8 +3,9 @@
 //   mean = 1/C sum x,  rstd = 1 / sqrt(1/C sum (x - mean)^2 + eps),  h = (x - mean) rstd,  y = h w + b
 //   g = dy w,  dx = rstd (g - 1/C sum g - h 1/C sum g h),  dw = sum over rows of dy h,  db = sum over rows of dy
 //
-// Statistics, products and sums are fp32; y and dx are rounded once.  The variance is summed around the mean, in a second pass over values
-// that are held in registers, so a row far from zero loses nothing.
+// Statistics, products and sums are fp32; y and dx are rounded once.  The forward pass sums a row, and then, over values that are held in registers, the
+// deviations from that mean and their squares: what is left of the mean, 1/C of the deviations' sum, is taken out of the mean, every deviation and the variance.
+// Without it a mean's rounding goes into all of a row's h, which the checkpoint scales up where they are small: 500 values of 1000.0 gave h = -0.02 each, and give 0.
 //
 // Both are bound by memory: a row is read once and held in registers by a group of 4 to 1024 lanes, eight columns (a chunk) of a lane
 // at a time.  The forward pass can write the checkpoint of h beside y, and the backward pass reads h from it (1.03 bytes a value) instead of x.
@@ -75,6 +76,13 @@ __device__ __forceinline__ float inverse_root(float v)
     return low ? r * 0x1p48f : r;
 }
 
+// Of the mean square around a mean, and what was left of that mean.  (Not below zero by a rounding; NaN stays.)
+__device__ __forceinline__ float variance(float square, float rest)
+{
+    const float v = __builtin_fmaf(-rest, rest, square);
+    return v < 0 ? 0.0f : v;
+}
+
 // Eight parameters of a chunk (n of them exist), in the element's type or in fp32; `none` where there are none.
 template <typename T> __device__ __forceinline__ void load_param(const void* p, bool f32, int64_t at, int n, float none, float v[8])
 {
@@ -120,7 +128,7 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForw
 {
     constexpr int W = LANES > 64 ? LANES / 64 : 1;
     constexpr bool MANY = many_rows(LANES, CH);
-    __shared__ float red[2][W];   // (a sum's words are written again behind the other sum's barrier)
+    __shared__ float red[3 * W];   // the first sum's words, the second's (written again behind the other sum's barrier)
     const int j = threadIdx.x % LANES;
     const int64_t first = (int64_t)blockIdx.x * Group<LANES>::ROWS;   // the workgroup's; `row` is that, or the wavefront's, and r the group's row behind it
     const int64_t row0 = first + Group<LANES>::mine();
@@ -157,9 +165,9 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForw
         }
         const int64_t next = row + (int64_t)gridDim.x * Group<LANES>::ROWS;
         if (MANY && next < a.rows) fetch(next);
-        group_sum<LANES, 1>(sum, red[0]);
+        group_sum<LANES, 1>(sum, red);
         const float mean = sum[0] * a.inv_cols;
-        sum[0] = 0;
+        float dev[2] = {0, 0};
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const int n = count(i);
@@ -170,13 +178,14 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForw
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 v[i][u] -= mean;
-                sum[0] = __builtin_fmaf(v[i][u], v[i][u], sum[0]);
+                dev[0] += v[i][u];
+                dev[1] = __builtin_fmaf(v[i][u], v[i][u], dev[1]);
             }
         }
-        group_sum<LANES, 1>(sum, red[1]);
-        const float rstd = inverse_root(sum[0] * a.inv_cols + a.eps);
+        group_sum<LANES, 2>(dev, red + W);
+        const float rest = dev[0] * a.inv_cols, rstd = inverse_root(variance(dev[1] * a.inv_cols, rest) + a.eps), shift = -rest * rstd;
         if (there && j == 0) {
-            if (a.mean) a.mean[row + r] = mean;
+            if (a.mean) a.mean[row + r] = mean + rest;
             if (a.rstd) a.rstd[row + r] = rstd;
         }
         T* const y = element(a.y, a.ldy, row, r, 0);
@@ -186,13 +195,17 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForw
             const int c = j + i * LANES, n = count(i);
             float h[8], o[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) h[u] = v[i][u] * rstd;
+            for (int u = 0; u < 8; ++u) h[u] = __builtin_fmaf(v[i][u], rstd, shift);
             if constexpr (!MANY) params(i, w[0], b[0]);
 #pragma unroll
             for (int u = 0; u < 8; ++u) o[u] = __builtin_fmaf(h[u], w[MANY ? i : 0][u], b[MANY ? i : 0][u]);
             row_store<RAGGED>(y, c, there ? n : 0, o);
             if (a.k.q) {
-                const uint32_t m = quad_max_u32(abs_max_bits(h)), e = ckpt_exponent(m);
+                if (RAGGED && n < 8) {   // columns that do not exist are nothing to a block's largest value
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) h[u] = u < n ? h[u] : 0.0f;
+                }
+                const uint32_t m = quad_max_u32(RAGGED || n > 0 ? abs_max_bits(h) : 0u), e = ckpt_exponent(m);
                 const u32x2 q = ckpt_codes(h, m, e, a.r, (uint64_t)row * (uint64_t)a.cols + ((uint64_t)r * (uint32_t)a.cols + 8 * (uint32_t)c));
                 if (there)
                     ckpt_store_chunk(a.k, element(a.k.q, a.k.pitch, row, r, 0), element(a.k.e, a.k.epitch, row, r, 0), c, LANES * CH, n > 0, q, e);
@@ -206,7 +219,7 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForw
 // Rows of more columns than a workgroup holds (32768): read three times, from the caches but for the first.
 template <typename T> __global__ __launch_bounds__(1024) void k_norm_forward_wide(NormForwardArgs<T> a)
 {
-    __shared__ float red[2][16];
+    __shared__ float red[3 * 16];
     const int64_t row = blockIdx.x;
     const T* const x = a.x + row * a.ldx;
     T* const y = a.y + row * a.ldy;
@@ -218,26 +231,29 @@ template <typename T> __global__ __launch_bounds__(1024) void k_norm_forward_wid
 #pragma unroll
         for (int u = 0; u < 8; ++u) sum[0] += v[u];
     }
-    group_sum<1024, 1>(sum, red[0]);
+    group_sum<1024, 1>(sum, red);
     const float mean = sum[0] * a.inv_cols;
     auto deviations = [&](int c, float v[8]) {
         const int n = max(0, min(8, a.cols - 8 * c));
         load8(x + 8 * c, n, v);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = u < n ? v[u] - mean : mean - mean;
+        for (int u = 0; u < 8; ++u) v[u] = u < n ? v[u] - mean : 0.0f;
         return n;
     };
-    sum[0] = 0;
+    float dev[2] = {0, 0};
     for (int c = threadIdx.x; c < chunks; c += 1024) {
         float v[8];
         deviations(c, v);
 #pragma unroll
-        for (int u = 0; u < 8; ++u) sum[0] = __builtin_fmaf(v[u], v[u], sum[0]);
+        for (int u = 0; u < 8; ++u) {
+            dev[0] += v[u];
+            dev[1] = __builtin_fmaf(v[u], v[u], dev[1]);
+        }
     }
-    group_sum<1024, 1>(sum, red[1]);
-    const float rstd = inverse_root(sum[0] * a.inv_cols + a.eps);
+    group_sum<1024, 2>(dev, red + 16);
+    const float rest = dev[0] * a.inv_cols, rstd = inverse_root(variance(dev[1] * a.inv_cols, rest) + a.eps), shift = -rest * rstd;
     if (threadIdx.x == 0) {
-        if (a.mean) a.mean[row] = mean;
+        if (a.mean) a.mean[row] = mean + rest;
         if (a.rstd) a.rstd[row] = rstd;
     }
     for (int c = threadIdx.x; c < chunks; c += 1024) {
@@ -247,7 +263,7 @@ template <typename T> __global__ __launch_bounds__(1024) void k_norm_forward_wid
         load_param<T>(a.bias, a.param_f32, 8 * c, n, 0.0f, b);
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
-            h[u] *= rstd;
+            h[u] = u < n ? __builtin_fmaf(h[u], rstd, shift) : 0.0f;
             o[u] = __builtin_fmaf(h[u], w[u], b[u]);
         }
         store8(y + 8 * c, n, o);
