@@ -133,23 +133,31 @@ template <typename T, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckp
     }
 }
 
-// f(u) and f'(u).  GELU: Phi(-|u|) = 1/2 t (a1 + t (a2 + ...)) exp(-u^2/2), t = 1 / (1 + p |u| / sqrt 2): Abramowitz and Stegun 7.1.26, off by at
-// most 0.75e-7 (about one unit of fp32 at 1), and its exponential is the density's too.  With more arithmetic than this the large case is bound by it and not by
-// memory: 16384 x 4096 bf16 values 96 us with the library's erf and exp, 62 to 65 this way.
-template <int ACT> __device__ __forceinline__ void act_of(float u, float& f, float& d)
+// f(u) and f'(u).  GELU's exponential is the density's as well as a factor of Phi(-|u|).
+// 16-bit values: Phi(-|u|) = 1/2 t (a1 + t (a2 + ...)) exp(-u^2/2), t = 1 / (1 + p |u| / sqrt 2): Abramowitz and Stegun 7.1.26, off by at most 0.75e-7, far
+// below their rounding of 2^-9 or 2^-12.  With more arithmetic than this the large case is bound by it and not by memory: 16384 x 4096 bf16 values 96 us with
+// the library's erf and exp, 62 to 65 this way.
+// fp32 values: that is more than the rounding of an fp32 product (rms of f' 9.7e-8 of its size, 4.1e-8 with erf), so Phi = 1/2 (1 + erf(u / sqrt 2)): 115 us for 16384 x 4096
+// values, 110 the other way.
+template <typename T, int ACT> __device__ __forceinline__ void act_of(float u, float& f, float& d)
 {
     if constexpr (ACT == FF_ACT_RELU) {
         f = u > 0 ? u : (u == u ? 0.0f : u);
         d = u > 0 ? 1.0f : (u == u ? 0.0f : u);
     } else if constexpr (ACT == FF_ACT_GELU) {
         const float e = __builtin_amdgcn_exp2f(u * u * -0.72134752044448170f);              // exp(-u^2 / 2)
-        const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(u), 0.23164189110f, 1.0f));   // p / sqrt 2
-        float q = __builtin_fmaf(t, 0.5307027145f, -0.7265760135f);                         // half of the polynomial
-        q = __builtin_fmaf(t, q, 0.7107068705f);
-        q = __builtin_fmaf(t, q, -0.142248368f);
-        q = __builtin_fmaf(t, q, 0.127414796f);
-        // Phi(u): 1 - low above zero, else low; a code that is not zero stands for 2^-106 at least
-        const float phi = __builtin_fabsf(__builtin_amdgcn_fmed3f(u * 0x1p127f, 0.0f, 1.0f) - t * q * e);
+        float phi;
+        if constexpr (sizeof(T) == 4) {
+            phi = __builtin_fmaf(0.5f, erff(u * 0.70710678118654752f), 0.5f);
+        } else {
+            const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(u), 0.23164189110f, 1.0f));   // p / sqrt 2
+            float q = __builtin_fmaf(t, 0.5307027145f, -0.7265760135f);                     // half of the polynomial
+            q = __builtin_fmaf(t, q, 0.7107068705f);
+            q = __builtin_fmaf(t, q, -0.142248368f);
+            q = __builtin_fmaf(t, q, 0.127414796f);
+            // Phi(u): 1 - low above zero, else low; a code that is not zero stands for 2^-106 at least
+            phi = __builtin_fabsf(__builtin_amdgcn_fmed3f(u * 0x1p127f, 0.0f, 1.0f) - t * q * e);
+        }
         f = u * phi;
         d = __builtin_fmaf(u * e, 0.39894228040143268f, phi);
     } else if constexpr (ACT == FF_ACT_SILU) {
@@ -200,7 +208,7 @@ template <typename T, int ACT, RowEnds ENDS, int U> __global__ __launch_bounds__
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             float f, d;
-            act_of<ACT>(u[j], f, d);
+            act_of<T, ACT>(u[j], f, d);
             // (c2 = 0 where there is no c: f is finite, or it is NaN and so is d, but for the identity's)
             v[j] = ACT == FF_ACT_IDENTITY && !a.coeff ? v[j] : __builtin_fmaf(c2, f, v[j]) * d;
         }
