@@ -278,7 +278,7 @@ template <typename T> __global__ __launch_bounds__(1024) void k_norm_forward_wid
 // ------------------------------------------------------------------------------------------------
 // Backward.  A workgroup keeps the column sums of its rows in registers (a lane's columns never change) and leaves them in the
 // workspace; k_norm_columns adds the workgroups' sums in order, so results do not depend on timing.  Of few rows, other workgroups of the same launch
-// make the column sums.
+// make the column sums (of a launch of their own, before it, where dx overwrites what they read).
 // ------------------------------------------------------------------------------------------------
 template <typename T> struct NormBackwardArgs {
     const T* dy;
@@ -732,7 +732,7 @@ size_t norm_backward_workspace(int64_t rows, int64_t cols)
     return n < FF_WS_MIN_BYTES ? FF_WS_MIN_BYTES : n;
 }
 
-template <typename T, bool KEPT, bool RAGGED> static void backward_as(const NormPlan& p, const NormBackwardArgs<T>& a, int64_t column_wgs, hipStream_t s)
+template <typename T, bool KEPT, bool RAGGED> static void backward_by(const NormPlan& p, const NormBackwardArgs<T>& a, int64_t column_wgs, hipStream_t s)
 {
     const dim3 grid((unsigned)(a.row_wgs + column_wgs));
     if (p.lanes == 4) k_norm_backward<T, KEPT, 4, 1, RAGGED><<<grid, 256, 0, s>>>(a);
@@ -746,6 +746,12 @@ template <typename T, bool KEPT, bool RAGGED> static void backward_as(const Norm
     else if (p.lanes == 256) k_norm_backward<T, KEPT, 256, 2, RAGGED><<<grid, 256, 0, s>>>(a);
     else if (p.ch == 2) k_norm_backward<T, KEPT, 512, 2, RAGGED><<<grid, 512, 0, s>>>(a);
     else k_norm_backward<T, KEPT, 512, 4, RAGGED><<<grid, 512, 0, s>>>(a);
+}
+template <typename T, bool KEPT> static hipError_t backward_as(const NormPlan& p, const NormBackwardArgs<T>& a, int64_t column_wgs, hipStream_t s)
+{
+    if (a.cols % 8 == 0) backward_by<T, KEPT, false>(p, a, column_wgs, s);
+    else backward_by<T, KEPT, true>(p, a, column_wgs, s);
+    return hipGetLastError();
 }
 template <typename T, bool KEPT> static hipError_t backward_of(const NormBackwardLaunch& l, hipStream_t s)
 {
@@ -772,20 +778,23 @@ template <typename T, bool KEPT> static hipError_t backward_of(const NormBackwar
     a.dweight = l.dweight;
     a.dbias = l.dbias;
     a.accumulate = l.accumulate;
-    const bool at_once = a.sums && sums_at_once(p, l.rows, l.cols) && l.dx != l.dy && (!l.x || l.dx != l.x);   // (in place, rows are written while columns are read)
-    const int64_t column_wgs = at_once ? (l.cols + 63) / 64 : 0;
-    a.row_wgs = at_once && !l.dx ? 0 : p.wgs;
+    const bool at_once = a.sums && sums_at_once(p, l.rows, l.cols);
+    const bool in_place = l.dx && (l.dx == l.dy || l.dx == l.x);
+    int64_t column_wgs = at_once ? (l.cols + 63) / 64 : 0;
     if (at_once) a.sums = 0;
+    if (at_once && (in_place || !l.dx)) {   // the columns alone; in place they are read before any row is written, and added in the same order as elsewhere
+        a.row_wgs = 0;
+        const hipError_t err = backward_as<T, KEPT>(p, a, column_wgs, s);
+        if (err != hipSuccess || !l.dx) return err;
+        column_wgs = 0;
+    }
+    a.row_wgs = p.wgs;
     if (l.rows > 0) {
         if (p.ch == 0) {
             if (a.dx) k_norm_row_sums<T, KEPT><<<dim3((unsigned)l.rows), 1024, 0, s>>>(a);
             k_norm_backward_wide<T, KEPT><<<dim3((unsigned)((a.cols + 2047) / 2048), (unsigned)p.wgs), 256, 0, s>>>(a);
-        } else if (a.cols % 8 == 0) {
-            backward_as<T, KEPT, false>(p, a, column_wgs, s);
-        } else {
-            backward_as<T, KEPT, true>(p, a, column_wgs, s);
         }
-        const hipError_t err = hipGetLastError();
+        const hipError_t err = p.ch == 0 ? hipGetLastError() : backward_as<T, KEPT>(p, a, column_wgs, s);
         if (err != hipSuccess) return err;
     }
     if (a.sums) {
