@@ -715,13 +715,21 @@ static NormPlan backward_plan(int64_t rows, int64_t cols)
     p.wgs = need < most ? need : most;
     return p;
 }
-// One launch for rows and columns, or the workgroups' sums and a launch that adds them.  bf16, us, one launch and two: 1 x 784 3.8 and 6.8, 128 x 784 3.7 and 7.1,
-// 128 x 16384 7.1 and 17.7, 256 x 500 5.8 and 7.0, 512 x 500 9.1 and 7.5, 512 x 784 5.5 and 7.6, 512 x 4096 6.3 and 16.2, 1024 x 784 8.7 and 8.6, 1024 x 4096
-// 11.8 and 17.6; fp32: 512 x 16384 32 and 34, 1024 x 16384 58 and 50.
-static bool sums_at_once(const NormPlan& p, int64_t rows, int64_t cols)
+// One launch for rows and columns, or the workgroups' sums and a launch that adds them.  One launch takes time by the rows that a column's workgroup reads, and
+// more where rows end inside a chunk, whose loads are behind branches; two are 6 to 20 us nearly whatever the rows.  us, one launch and two, on both sides of the lines:
+//   whole chunks        512 x 256 fp32 5.3 and 5.6, 640 x 256 6.0 and 5.9; 768 x 784 fp32 7.5 and 8.1, 768 x 12000 34 and 33, 768 x 16384 45 and 41,
+//                       1024 x 784 9.8 and 8.8;
+//     up to 16 KB       1024 x 2000 bf16 10.5 and 12.9, 1024 x 4096 fp32 17 and 18, 1024 x 8192 bf16 17.4 and 18.2; beyond: 1024 x 6000 fp32 24 and 21
+//   ragged, from x      256 x 783 fp32 7.2 and 7.6, 320 x 783 8.7 and 8.0; 448 x 2001 fp32 11.6 and 12.7, 512 x 2001 14.4 and 13.3, 1024 x 2001 33 and 15; bf16
+//                       512 x 2001 11.5 and 13.8, 640 x 3001 19 and 16
+//   ragged, from codes  384 x 500 fp32 6.1 and 6.3, 448 x 500 6.6 and 6.4; 384 x 783 7.1 and 7.6, 512 x 783 8.5 and 7.8; 640 x 2001 fp32 11.8 and 14.0, 768 x 2001 14.5 and 14.1; bf16 768 x 2001 10.9 and 13.5,
+//                       1024 x 2001 13.6 and 13.2
+static bool sums_at_once(const NormPlan& p, int64_t rows, int64_t cols, int size, bool kept)
 {
     if (p.ch == 0 || rows == 0) return false;
-    return rows <= 256 || (rows <= 512 && cols > 512) || (rows <= 1024 && cols >= 2000 && cols <= 8192);
+    if (cols % 8 == 0) return rows <= 512 || (rows <= 768 && cols > 512 && cols * size <= 49152) || (rows <= 1024 && cols > 1024 && cols * size <= 16384);
+    if (cols <= 1024) return rows <= (kept ? (cols > 512 ? 448 : 384) : 256);
+    return rows <= (kept ? (size == 2 ? 768 : 640) : (size == 2 ? 512 : 448));
 }
 static int64_t padded_cols(int64_t cols) { return (cols + 7) / 8 * 8; }
 size_t norm_backward_workspace(int64_t rows, int64_t cols)
@@ -778,7 +786,7 @@ template <typename T, bool KEPT> static hipError_t backward_of(const NormBackwar
     a.dweight = l.dweight;
     a.dbias = l.dbias;
     a.accumulate = l.accumulate;
-    const bool at_once = a.sums && sums_at_once(p, l.rows, l.cols);
+    const bool at_once = a.sums && sums_at_once(p, l.rows, l.cols, sizeof(T), KEPT);
     const bool in_place = l.dx && (l.dx == l.dy || l.dx == l.x);
     int64_t column_wgs = at_once ? (l.cols + 63) / 64 : 0;
     if (at_once) a.sums = 0;
