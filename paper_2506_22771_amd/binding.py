@@ -301,8 +301,8 @@ def ff_train_step_at(net: Net, x_pos, x_neg, theta, lam, lr, seed, step_dev, adv
 
 
 # --- layer norm and 8-bit checkpoints.  Matrices are 2-D tensors of float32, bfloat16 or float16 with consecutive columns and any row
-# stride (a view of some columns of a wider tensor will do).  Shapes, types, strides and devices are compared with each other (ValueError),
-# because the library sees addresses and sizes only; that and the marshalling are compiled (csrc/bind.cpp).
+# stride (a view of some columns of a wider tensor will do).  Shapes, types, strides and devices are compared with each other, and the device with the
+# current one, whose stream is used (ValueError), because the library sees addresses and sizes only; that and the marshalling are compiled (csrc/bind.cpp).
 _bind = None
 
 

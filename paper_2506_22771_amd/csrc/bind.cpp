@@ -1,10 +1,11 @@
-// Python's side of the layer norm and checkpoint calls: shapes, types, strides and devices of the tensors are compared here and
-// their addresses handed to the library.  Marshalling only, in C++ because these calls are short: a norm of one 4096-wide row took 8.3 us through
+// Python's side of the layer norm and checkpoint calls: shapes, types, strides and devices of the tensors are compared here (all lie on the current
+// device, whose stream the work goes to) and their addresses handed to the library.  Marshalling only, in C++ because these calls are short: a norm of one 4096-wide row took 8.3 us through
 // ctypes, nearly all of it spent on attributes and argument conversions in Python.
 //
 // Tensors of the wrong shape, type, stride or device raise ValueError; the library's own refusals come back as its status.
 #include <Python.h>
 
+#include <c10/core/impl/DeviceGuardImplInterface.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <initializer_list>
@@ -37,6 +38,27 @@ const at::Tensor& tensor(PyObject* o, const char* what)
 void on_device(const at::Tensor& t, const char* what)
 {
     if (!t.is_cuda()) refuse(what, "device tensor");
+}
+// Of all arguments that are device tensors.  (What else there is among them is refused by its own name.)
+void one_device(PyObject* const* a, int n)
+{
+    int first = -1;
+    for (int i = 0; i < n; ++i) {
+        if (!THPVariable_Check(a[i])) continue;
+        const at::Device d = THPVariable_Unpack(a[i]).device();
+        if (!d.is_cuda()) continue;
+        if (first >= 0 && d.index() != first) {
+            PyErr_Format(PyExc_ValueError, "tensors on one device expected, got cuda:%d and cuda:%d", first, (int)d.index());
+            throw Refused();
+        }
+        first = d.index();
+    }
+    if (first < 0) return;
+    const int current = c10::impl::getDeviceGuardImpl(c10::DeviceType::CUDA)->getDevice().index();
+    if (first != current) {
+        PyErr_Format(PyExc_ValueError, "tensors on the current device, cuda:%d, expected, got cuda:%d", current, first);
+        throw Refused();
+    }
 }
 
 int32_t kind_of(at::ScalarType t) { return t == at::kFloat ? FF_F32 : t == at::kBFloat16 ? FF_BF16 : t == at::kHalf ? FF_F16 : -1; }
@@ -174,6 +196,7 @@ template <int N, typename F> PyObject* call(PyObject* const* a, Py_ssize_t n, F&
         return nullptr;
     }
     try {
+        one_device(a, N);
         return PyLong_FromLong(f(a));
     } catch (const Refused&) {
         return nullptr;
