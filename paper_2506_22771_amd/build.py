@@ -2,7 +2,8 @@
 
     python -m paper_2506_22771_amd.build [--force]
 
-and _bind.so, the compiled marshalling of the layer norm and checkpoint calls (host code, against torch's headers), with g++.
+and _bind.so, the compiled marshalling of Python's layer norm and checkpoint calls (host code, against Python's and torch's headers), with g++.
+Where one of these is not there the library is built all the same, for its C interface and the other Python calls; what is missing is printed.
 
 -ffp-contract=off: the numerics need one rounding per written fp32 operation (hipcc would fuse).
 -packed-fp32-ops is switched off as required on the test machines."""
@@ -11,6 +12,7 @@ from __future__ import annotations
 import concurrent.futures as cf
 import importlib.util
 import os
+import shutil
 import subprocess
 import sys
 import sysconfig
@@ -43,14 +45,29 @@ def _compile(src: str, force: bool) -> str:
     return obj
 
 
+def _bind_needs() -> dict:
+    """What building _bind.so takes, and where it is (None: not there)."""
+    spec = importlib.util.find_spec("torch")   # (without importing it)
+    torch = os.path.join(os.path.dirname(spec.origin), "include") if spec and spec.origin else None
+    python = sysconfig.get_paths()["include"]
+    return {"g++": shutil.which("g++"), "Python's headers": python if os.path.exists(os.path.join(python, "Python.h")) else None,
+            "torch's headers": torch if torch and os.path.exists(os.path.join(torch, "torch", "csrc", "autograd", "python_variable.h")) else None}
+
+
 def _build_bind(force: bool) -> None:
     src = os.path.join(CSRC, "bind.cpp")
     if not (force or _stale(BIND, [src, LIB, HEADERS[-1]])):
         return
-    torch = os.path.join(os.path.dirname(importlib.util.find_spec("torch").origin))   # (without importing it)
-    subprocess.run(["g++", "-O2", "-fPIC", "-shared", "-std=c++17", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=1",
-                    "-I" + os.path.join(torch, "include"), "-I" + os.path.join(torch, "include", "torch", "csrc", "api", "include"),
-                    "-I" + sysconfig.get_paths()["include"], src, "-o", BIND + ".tmp", "-L" + os.path.join(torch, "lib"),
+    needs = _bind_needs()
+    missing = [what for what, where in needs.items() if where is None]
+    if missing:
+        if os.path.exists(BIND):
+            os.remove(BIND)     # (it is older than the library)
+        print(f"_bind.so is not built ({', '.join(missing)} not found): no layer norm and checkpoint calls from Python", file=sys.stderr)
+        return
+    torch = needs["torch's headers"]
+    subprocess.run([needs["g++"], "-O2", "-fPIC", "-shared", "-std=c++17", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=1", "-I" + torch, "-I" + os.path.join(torch, "torch", "csrc", "api", "include"),
+                    "-I" + needs["Python's headers"], src, "-o", BIND + ".tmp", "-L" + os.path.join(os.path.dirname(torch), "lib"),
                     "-ltorch_python", "-ltorch_cpu", "-lc10", "-L" + HERE, "-l:libffint8.so", "-Wl,-rpath,$ORIGIN"], check=True)
     os.replace(BIND + ".tmp", BIND)
 
