@@ -37,14 +37,9 @@ __device__ __forceinline__ void chunk_place(const Chunks& c, uint32_t chunk0, ui
 }
 __device__ __forceinline__ void chunk_first(const Chunks& c, int64_t first, int64_t& row0, uint32_t& chunk0)
 {
-    if (first >> 32) {
-        row0 = first / c.slots;
-        chunk0 = (uint32_t)(first - row0 * c.slots);
-    } else {
-        const uint32_t r = (uint32_t)first / c.slots;
-        row0 = r;
-        chunk0 = (uint32_t)first - r * c.slots;
-    }
+    const uint32_t r = (uint32_t)first / c.slots;   // (a matrix has fewer than 2^31 chunks: size_status)
+    row0 = r;
+    chunk0 = (uint32_t)first - r * c.slots;
 }
 
 template <typename T> struct CkptArgs {
