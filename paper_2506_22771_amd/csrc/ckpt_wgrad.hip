@@ -407,33 +407,34 @@ __global__ __launch_bounds__(128 * WK) __attribute__((amdgpu_waves_per_eu(BT == 
     }
 }
 
-// Adds the splits' results in order, four values a thread: dw, then db.  No splits (no rows): zero.
+// Adds the splits' results in order, four values a thread and round: dw, then db.  No splits (no rows): zero.
 __global__ __launch_bounds__(256) void k_ckpt_wgrad_sum(WgradArgs a)
 {
-    const int64_t size = (int64_t)a.n * a.k, at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, end = size + (a.db ? a.n : 0);
-    if (at >= end) return;
-    float4 v = make_float4(0, 0, 0, 0);
-    const float* p = a.part + at;   // (a split's results are followed by room up to `stride`, a multiple of four)
+    const int64_t size = (int64_t)a.n * a.k, end = size + (a.db ? a.n : 0);
+    for (int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; at < end; at += (int64_t)gridDim.x * 1024) {
+        float4 v = make_float4(0, 0, 0, 0);
+        const float* p = a.part + at;   // (a split's results are followed by room up to `stride`, a multiple of four)
 #pragma unroll 4
-    for (int s = 0; s < a.splits; ++s, p += a.stride) {
-        const float4 t = *(const float4*)p;
-        v = make_float4(v.x + t.x, v.y + t.y, v.z + t.z, v.w + t.w);
-    }
-    const float r[4] = {v.x, v.y, v.z, v.w};
-    if (at + 4 <= size) {
-        float* const to = a.dw + at;
-        u32x4 o;
-        if (a.accumulate) o = read_as<u32x4>(to);
+        for (int s = 0; s < a.splits; ++s, p += a.stride) {
+            const float4 t = *(const float4*)p;
+            v = make_float4(v.x + t.x, v.y + t.y, v.z + t.z, v.w + t.w);
+        }
+        const float r[4] = {v.x, v.y, v.z, v.w};
+        if (at + 4 <= size) {
+            float* const to = a.dw + at;
+            u32x4 o;
+            if (a.accumulate) o = read_as<u32x4>(to);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = __float_as_uint(a.accumulate ? __uint_as_float(o[i]) + r[i] : r[i]);
-        write_as<u32x4>(to, o);
-    } else {
+            for (int i = 0; i < 4; ++i) o[i] = __float_as_uint(a.accumulate ? __uint_as_float(o[i]) + r[i] : r[i]);
+            write_as<u32x4>(to, o);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (at + i < end) {
-                float* const to = at + i < size ? a.dw + at + i : a.db + (at + i - size);
-                *to = a.accumulate ? *to + r[i] : r[i];
-            }
+            for (int i = 0; i < 4; ++i)
+                if (at + i < end) {
+                    float* const to = at + i < size ? a.dw + at + i : a.db + (at + i - size);
+                    *to = a.accumulate ? *to + r[i] : r[i];
+                }
+        }
     }
 }
 
@@ -487,8 +488,9 @@ template <typename T> static hipError_t wgrad_of(const CkptWgradLaunch& l, hipSt
         if (err != hipSuccess) return err;
     }
     if (a.splits != 1) {
-        const int64_t all = (int64_t)a.n * a.k + a.n;
-        k_ckpt_wgrad_sum<<<dim3((unsigned)((all + 1023) / 1024)), 256, 0, s>>>(a);
+        // (one round of the sum for all that is split; dw may have more elements than a launch has lanes for where there are no rows)
+        const int64_t all = (int64_t)a.n * a.k + a.n, wgs = (all + 1023) / 1024, most = int64_t(1) << 20;
+        k_ckpt_wgrad_sum<<<dim3((unsigned)(wgs < most ? wgs : most)), 256, 0, s>>>(a);
         return hipGetLastError();
     }
     return hipSuccess;
