@@ -80,8 +80,7 @@ Mat matrix(PyObject* o, const char* what)
     m.rows = t.size(0);
     m.cols = t.size(1);
     on_device(t, what);
-    m.ld = t.stride(0);
-    if (m.rows <= 1 && m.ld < m.cols) m.ld = m.cols;
+    m.ld = m.rows <= 1 ? m.cols : t.stride(0);   // (of one row it says nothing)
     if ((t.stride(1) != 1 && m.cols > 1) || m.ld < m.cols) refuse(what, "consecutive columns and rows that do not overlap, as a matrix", m.rows, m.cols);
     m.p = t.data_ptr();
     return m;
