@@ -6,6 +6,8 @@
 // Statistics, products and sums are fp32; y and dx are rounded once.  The forward pass sums a row, and then, over values that are held in registers, the
 // deviations from that mean and their squares: what is left of the mean, 1/C of the deviations' sum, is taken out of the mean, every deviation and the variance.
 // Without it a mean's rounding goes into all of a row's h, which the checkpoint scales up where they are small: 500 values of 1000.0 gave h = -0.02 each, and give 0.
+// That is for rows farther from zero than they are wide.  There the deviations are exact or nearly; elsewhere their own roundings are more than what the first sum
+// lacks, and the mean stays as it is.
 //
 // Both are bound by memory: a row is read once and held in registers by a group of 4 to 1024 lanes, eight columns (a chunk) of a lane
 // at a time.  The forward pass can write the checkpoint of h beside y, and the backward pass reads h from it (1.03 bytes a value) instead of x.
@@ -76,7 +78,8 @@ __device__ __forceinline__ float inverse_root(float v)
     return low ? r * 0x1p48f : r;
 }
 
-// Of the mean square around a mean, and what was left of that mean.  (Not below zero by a rounding; NaN stays.)
+// What is left of a row's mean, by the mean of the deviations from it and that of their squares; and the variance.  (Not below zero by a rounding; NaN stays.)
+__device__ __forceinline__ float mean_rest(float mean, float deviation, float square) { return mean * mean > square ? deviation : 0.0f; }
 __device__ __forceinline__ float variance(float square, float rest)
 {
     const float v = __builtin_fmaf(-rest, rest, square);
@@ -183,7 +186,8 @@ __global__ __launch_bounds__(Group<LANES>::THREADS) void k_norm_forward(NormForw
             }
         }
         group_sum<LANES, 2>(dev, red + W);
-        const float rest = dev[0] * a.inv_cols, rstd = inverse_root(variance(dev[1] * a.inv_cols, rest) + a.eps), shift = -rest * rstd;
+        const float square = dev[1] * a.inv_cols, rest = mean_rest(mean, dev[0] * a.inv_cols, square);
+        const float rstd = inverse_root(variance(square, rest) + a.eps), shift = -rest * rstd;
         if (there && j == 0) {
             if (a.mean) a.mean[row + r] = mean + rest;
             if (a.rstd) a.rstd[row + r] = rstd;
@@ -251,7 +255,8 @@ template <typename T> __global__ __launch_bounds__(1024) void k_norm_forward_wid
         }
     }
     group_sum<1024, 2>(dev, red + 16);
-    const float rest = dev[0] * a.inv_cols, rstd = inverse_root(variance(dev[1] * a.inv_cols, rest) + a.eps), shift = -rest * rstd;
+    const float square = dev[1] * a.inv_cols, rest = mean_rest(mean, dev[0] * a.inv_cols, square);
+    const float rstd = inverse_root(variance(square, rest) + a.eps), shift = -rest * rstd;
     if (threadIdx.x == 0) {
         if (a.mean) a.mean[row] = mean + rest;
         if (a.rstd) a.rstd[row] = rstd;
