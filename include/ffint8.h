@@ -400,7 +400,7 @@ size_t ff_workspace_bytes(const ff_net_desc* net);
  *
  * Matrices of floating-point values in this part
  *  - [rows, cols], element type `dtype` (FF_F32, FF_BF16 or FF_F16), consecutive columns, rows `ld` ELEMENTS apart,
- *    ld >= cols; base addresses aligned to the element.  Arithmetic is fp32 whatever the type; results are rounded once.
+ *    cols <= ld <= 2^31; base addresses aligned to the element.  Arithmetic is fp32 whatever the type; results are rounded once.
  *  - 1 <= cols <= 2^24 and 0 <= rows < 2^31 (FF_ERR_SHAPE / FF_ERR_UNSUPPORTED); fewer than 2^34 elements, columns counted in whole
  *    rows of codes (ff_pitch(cols), rounded up to whole blocks), else FF_ERR_UNSUPPORTED.
  *  - rows == 0 is accepted: matrix pointers may be NULL then, sums over rows are zero.
@@ -438,7 +438,7 @@ ff_status ff_layer_norm_forward(int64_t rows, int64_t cols, int32_t dtype, int32
  *   dx [rows, cols] of type dtype, dweight and dbias fp32 [cols]: any may be NULL, not all three.
  *   accumulate: 1 adds to dweight and dbias, 0 overwrites them.
  *   ws: >= ff_layer_norm_workspace_bytes(rows, cols) bytes, 16-byte aligned.
- * Sums are formed in a fixed order: equal inputs give equal bits. */
+ * Sums are formed in a fixed order, whatever else is asked for and also in place: equal inputs give equal bits. */
 size_t ff_layer_norm_workspace_bytes(int64_t rows, int64_t cols);   /* 0 for sizes that are refused. [host only] */
 ff_status ff_layer_norm_backward(int64_t rows, int64_t cols, int32_t dtype, int32_t param_dtype, const void* dy,
                                  int64_t lddy, const void* x, int64_t ldx, const float* mean, const int8_t* q,

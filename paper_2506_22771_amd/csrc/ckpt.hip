@@ -4,8 +4,8 @@
 //   act backward:  dx = (dy + 2 c[row] f(u)) f'(u), u the checkpointed argument of f; 2 c f(u) is the gradient of c G, the goodness
 //                  G = sum f(u)^2 of Section III (dL/dG = c), dy what comes down from the layers above (either may be absent)
 //
-// Measured, us and TB/s, 16384 x 4096 (a copy of as many bytes reaches 5.3): bf16 store 31 (6.5), with stochastic rounding 43-48 (4.5, by its arithmetic:
-// 25 operations a value), load 30 (6.8), GELU backward 62-65 (5.3); fp32 60 (5.6), 63 (5.4), 71 (4.8), 110 (5.5).
+// Measured, us and TB/s, 16384 x 4096, inputs from memory (a copy of as many bytes reaches 5.3): bf16 store 41 (4.9), with stochastic rounding 53 (3.8, by its
+// arithmetic: 25 operations a value), load 38 (5.3), ReLU backward 59 (5.7), GELU 64 (5.3); fp32 60 (5.6), 63 (5.3), 69 (4.9), 108 (5.6), 114 (5.3).
 // All three are bound by memory but for that.  A lane has eight columns (a chunk) of a row, a quad of lanes one block; a workgroup takes consecutive chunks,
 // whatever the row length, and has all its loads in flight before the first is used.
 #include <type_traits>

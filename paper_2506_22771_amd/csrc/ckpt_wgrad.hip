@@ -14,10 +14,10 @@
 // they lie, and the fragments are read with the transposing LDS read.  Three stages of LDS: while a step is multiplied the one after the next is
 // written and the first fragments of the next are read already, so that no wavefront waits for LDS behind the barrier; registers hold the step after those.
 //
-// Bound by the matrix pipe and, in the large case, by what the card sustains of it.  Measured: 16384 rows, 4096 x 4096, bf16 519 to 543 us, 1.01 to
-// 1.06 PFLOP/s (a library product of bf16 matrices, both in memory already, 513 to 560); 2048 rows, 2000 x 2000, fp32 72 us, of which 12 add the splits: 0.68
-// PFLOP/s of the three bf16 products (a library product of fp32 matrices 123, one of bf16 matrices 29); 128 rows, 500 x 784, fp32 7.5, a launch with its first
-// loads.
+// Bound by the matrix pipe and, in the large case, by what the card sustains of it.  Measured: 16384 rows, 4096 x 4096, bf16 511 to 560 us, 0.98 to
+// 1.08 PFLOP/s (a library product of bf16 matrices, both in memory already, 513 to 560); 2048 rows, 2000 x 2000, fp32 72 to 77 us, of which 12 add the splits: 0.68
+// PFLOP/s of the three bf16 products (a library product of fp32 matrices 123, one of bf16 matrices 29); 128 rows, 500 x 784, fp32 7.5: 104
+// workgroups of 64 x 64 outputs on 256 compute units, four steps one after the other.
 #include <type_traits>
 
 #include "ckpt.hpp"

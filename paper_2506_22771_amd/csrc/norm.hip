@@ -12,14 +12,15 @@
 // Both are bound by memory: a row is read once and held in registers by a group of 4 to 1024 lanes, eight columns (a chunk) of a lane
 // at a time.  The forward pass can write the checkpoint of h beside y, and the backward pass reads h from it (1.03 bytes a value) instead of x.
 //
-// Measured, us and TB/s (a copy of as many bytes reaches 5.3):
+// Measured, us and TB/s, inputs from memory (a copy of as many bytes reaches 5.3):
 //                                    16384 x 4096 bf16    16384 x 4096 fp32    131072 x 784 bf16    262144 x 128 fp16
-//   forward                              45   6.0              98   5.4              82   5.0              23   5.9
-//   forward, codes to nearest            62   5.4             113   5.4             111   4.6              30   5.7
-//   forward, stochastic codes         67-77   4.7             115   5.3             130   4.0              44   3.8
-//   backward from x                      81   5.0             156   5.1             146   4.2              41   5.0
-//   backward from the checkpoint      70-81   4.5             118   5.1             135   3.8              36   4.7
-// Stochastic codes of 16-bit values are as much arithmetic as memory: some 30 operations a value, of which the random word takes ten.
+//   forward                              51   5.2              99   5.4              83   4.9              29   4.6
+//   forward, codes to nearest            67   5.0             114   5.3             111   4.7              40   4.3
+//   forward, stochastic codes         72-76   4.5             116   5.2             129   4.0              51   3.3
+//   backward from x                      80   5.0             159   5.1             146   4.2              50   4.0
+//   backward from the checkpoint         70   4.8             118   5.1             136   3.8              41   4.2
+// Stochastic codes of 16-bit values are as much arithmetic as memory: 38 operations a value, of which the random word takes ten.  784 columns are 98 chunks on
+// 64 lanes with two each: a quarter of what is issued works on columns that do not exist.
 #include <type_traits>
 
 #include "ckpt.hpp"
@@ -673,7 +674,9 @@ template <typename T> static hipError_t forward_of(const NormForwardLaunch& l, h
     a.r = {make_sr_key(l.seed, l.tag), l.round_mode == FF_ROUND_STOCHASTIC};
     // Lanes of a row: as few as hold it in two chunks each, since a wavefront's own sums need no barrier and fewer lanes are left over (131072 x 784
     // bf16, stochastic codes: 359 us by 256 lanes with a chunk each, 129 by 64; 32768 x 2000: 101 by 256, 74 by 128), and the smallest power of two for
-    // one chunk below that.
+    // one chunk below that.  (Of few rows one chunk a lane, half as many rows at once, is faster: 512 x 784 fp32 3.7 us by this and 3.4 by 128 lanes, 64 x 1001
+    // bf16 with stochastic codes 4.8 and 3.7, 1024 x 2000 fp32 5.4 and 5.3; 2048 x 2000 8.9 both with codes to nearest, 9.2 and 10.7 with stochastic ones.
+    // The rows are not asked.)
     const int64_t chunks = (a.k.pitch / 8 + 3) / 4 * 4;   // (pad columns of the checkpoint included)
     if (chunks <= 4) return forward_as<T, 4, 1>(a, s);
     if (chunks <= 8) return forward_as<T, 8, 1>(a, s);
