@@ -132,7 +132,7 @@ def test_elements_beyond_32_bits_of_index():
 
 
 # dx = (dy + 2 c f) f': f and f' are fp32 functions, good to a few units in the last place of the largest term they are made of: 1 for sigma and Phi,
-# |u| for f.  erf and exp of the device's library are within 4 units; twelve roundings follow at most.
+# |u| for f.  Phi is off by 1.3 U for 16-bit values and U / 14 for fp32 by its approximation, exp2 and rcp by a unit each; twelve roundings follow at most.
 def act_bound(kind, u, coeff, dy, dtype):
     f, d = N.act(kind, u)
     up = np.abs(dy if dy is not None else 0.0) + (2 * np.abs(coeff[:, None] * f) if coeff is not None else 0.0)

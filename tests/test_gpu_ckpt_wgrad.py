@@ -24,7 +24,7 @@ def checkpoint(rows, k, seed):
     return rq, re, *padded_ckpt(rq, re)
 
 
-# from one row to several splits of the rows; every tile; n and k at both sides of tiles, chunks and blocks
+# from one row to several splits of the rows; n and k at both sides of tiles, chunks and blocks (all by the tile of 64 outputs; test_gpu_ckpt_wgrad_tiles.py has the others)
 SHAPES = [(1, 1, 1), (1, 5, 33), (2, 300, 7), (31, 8, 32), (32, 64, 64), (33, 65, 63), (64, 100, 257), (100, 129, 40), (128, 500, 784), (65, 640, 650), (1000, 3, 2),
           (777, 17, 1000), (2048, 200, 96), (5000, 70, 130), (40000, 24, 32), (300, 1100, 1030)]
 
