@@ -478,6 +478,72 @@ ff_status ff_ckpt_weight_grad(const void* dy, int32_t dtype, int64_t lddy, const
                               float* db, int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Gated layers, group norm and dropout.  What else stands between two contractions of a trained stack: a layer whose activities are the product
+ * of two projections, a norm for maps, and the regulariser.  Matrices of floating-point values, checkpoints and activations (FF_ACT_*) as in the part above;
+ * `goodness` is the sum of a row's or a sample's squared activities (Section III) before they are rounded, `coeff` its loss derivative (dL/dG).
+ * ------------------------------------------------------------------------------------------- */
+
+/* ff_gated_forward — a gated layer in one kernel: with s = s_a s_w,
+ *   g[m][j] = s * sum_k a_q[m][k] * w_q[j][k],   u[m][j] = s * sum_k a_q[m][k] * w_q[n + j][k],   y = act(g) * u
+ *   a_q            int8 [rows, ff_pitch(k)]; rows <= 8388480
+ *   w_q            int8 [2n, ff_pitch(k)], the gate's rows first, one tensor to ff_quantize; 2n <= 65535.  FF_ERR_OVERFLOW_BOUND if k * 127^2 could exceed int32
+ *   s_a, s_w       device scalars
+ *   y              [rows, n], type dtype, rows ldy elements apart (out)
+ *   goodness       fp32 [rows]: sum over the row of y^2 (out, may be NULL)
+ *   qg, eg, qu, eu checkpoints of g and u, rounded to nearest (out, all four or none): what ff_gated_backward reads
+ *   ws             >= ff_gated_workspace_bytes(rows, n, k) bytes, 16-byte aligned
+ * Accumulators are exact; g and u are rounded twice (to fp32, by the scale).  Sums are formed in a fixed order: equal inputs give equal bits. */
+size_t ff_gated_workspace_bytes(int64_t rows, int64_t n, int64_t k);   /* 0 for sizes that are refused. [host only] */
+ff_status ff_gated_forward(int64_t rows, int64_t n, int64_t k, const int8_t* a_q, const int8_t* w_q, const float* s_a, const float* s_w, int32_t act,
+                           void* y, int32_t dtype, int64_t ldy, float* goodness, int8_t* qg, uint8_t* eg, int8_t* qu, uint8_t* eu, void* ws,
+                           size_t ws_bytes, void* stream);
+
+/* ff_gated_backward — gradient through the activation and the product, from the checkpoints of g and u:
+ *   t = dy + 2 * coeff[row] * act(g) * u,   dg = t * u * act'(g),   du = t * act(g)
+ * coeff (fp32 [rows]) or dy may be NULL, not both: that term is absent.  dg and du [rows, n] have a row stride each and may be the halves of one [rows, 2n] matrix
+ * (ff_ckpt_weight_grad then gives the gradient of w_q's matrix in one call, and ff_layer_input_grad over 2n features that of the layer's input); one of them
+ * may be dy itself. */
+ff_status ff_gated_backward(const int8_t* qg, const uint8_t* eg, const int8_t* qu, const uint8_t* eu, int64_t rows, int64_t n, int32_t act,
+                            const float* coeff, const void* dy, int64_t lddy, void* dg, int64_t lddg, void* du, int64_t lddu, int32_t dtype,
+                            void* stream);
+
+/* ff_group_norm_forward — norm over groups of channels of channels-last maps, with the activation behind it.  A map is a matrix
+ * [samples * pixels, channels]; a group is channels / groups consecutive channels (groups divides channels, channels <= 65535).  Per sample and group, over
+ * all its values: mean, rstd = 1 / sqrt(mean of (x - mean)^2 + eps), h = (x - mean) * rstd; then
+ *   y = act(h * weight + bias)
+ *   weight, bias  [channels], type param_dtype (FF_F32 or dtype), either may be NULL (1 and 0)
+ *   mean, rstd    fp32 [samples, groups] (out, either may be NULL)
+ *   goodness      fp32 [samples]: sum over the sample of y^2 (out, may be NULL)
+ *   q, e          checkpoint of h (out, both or neither), rounded by round_mode, seed and stream_tag
+ *   ws            >= ff_group_norm_workspace_bytes(samples, pixels, channels, groups) bytes, 16-byte aligned
+ * samples == 0 is accepted; pixels == 0 is FF_ERR_SHAPE. */
+size_t ff_group_norm_workspace_bytes(int64_t samples, int64_t pixels, int64_t channels, int64_t groups);   /* 0 for sizes that are refused. [host only] */
+ff_status ff_group_norm_forward(int64_t samples, int64_t pixels, int64_t channels, int64_t groups, int32_t dtype, int32_t param_dtype, const void* x,
+                                int64_t ldx, const void* weight, const void* bias, float eps, int32_t act, void* y, int64_t ldy, float* mean,
+                                float* rstd, float* goodness, int8_t* q, uint8_t* e, int32_t round_mode, uint64_t seed, uint64_t stream_tag,
+                                void* ws, size_t ws_bytes, void* stream);
+
+/* ff_group_norm_backward — with z = h * weight + bias, dz = (dy + 2 * coeff[sample] * act(z)) * act'(z), g = dz * weight, and <.> the mean over a group:
+ *   dx = rstd * (g - <g> - h * <g h>);  dweight = sum over samples and pixels of dz h;  dbias = sum over samples and pixels of dz
+ *   h comes from x, mean and rstd, as (x - mean) * rstd in fp32, or, with x == NULL, from the checkpoint q, e (mean is not read then).
+ *   dy or coeff (fp32 [samples]) may be NULL, not both.  dx of type dtype, dweight and dbias fp32 [channels]: any may be NULL, not all three.
+ *   accumulate: 1 adds to dweight and dbias, 0 overwrites them.  ws as above.  samples == 0: sums are zero.
+ * Sums are formed in a fixed order: equal inputs give equal bits. */
+ff_status ff_group_norm_backward(int64_t samples, int64_t pixels, int64_t channels, int64_t groups, int32_t dtype, int32_t param_dtype, const void* dy,
+                                 int64_t lddy, const float* coeff, const void* x, int64_t ldx, const float* mean, const int8_t* q, const uint8_t* e,
+                                 const float* rstd, const void* weight, const void* bias, int32_t act, void* dx, int64_t lddx, float* dweight,
+                                 float* dbias, int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* ff_dropout — y = r + (u >= p ? x / (1 - p) : 0), u the uniform of element row*cols+col under (seed, stream_tag): the random word of ff_quantize, of
+ * which no mask is kept.  The backward pass is the same call on the gradient, without r.
+ *   r        [rows, cols], added (may be NULL)
+ *   p        0 <= p <= 1; p == 1 drops everything.  What is dropped is zero whatever it was.
+ *   step_dev one uint64 in DEVICE memory (8-byte aligned) or NULL: the tag is stream_tag + (*step_dev << 20), that of step *step_dev where stream_tag is
+ *            ff_stream_tag(0, ...).  Read when the kernel runs: a captured call drops other elements at every replay that has advanced it. */
+ff_status ff_dropout(int64_t rows, int64_t cols, int32_t dtype, const void* x, int64_t ldx, const void* r, int64_t ldr, float p, uint64_t seed,
+                     uint64_t stream_tag, const uint64_t* step_dev, void* y, int64_t ldy, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Instrumentation (not part of the method).  ff_timing_enable(class_mask): bit c of the mask
  * selects kernel class c (-1 = every class, 0 = off).  Every launch of a selected class is
  * bracketed by a pair of HIP events recorded on the launch stream; ff_timing_read waits for the
@@ -505,7 +571,10 @@ enum {
     FF_K_NORM = 13,      /* layer norm, forward and backward: one record a call, as for the two below */
     FF_K_CKPT = 14,      /* 8-bit checkpoints written, read, and read by an activation's gradient */
     FF_K_CKPT_DW = 15,   /* weight gradient from a checkpoint */
-    FF_K_COUNT = 16
+    FF_K_GATED = 16,     /* gated layers, forward and backward */
+    FF_K_GROUP_NORM = 17, /* group norm, forward and backward  */
+    FF_K_DROPOUT = 18,
+    FF_K_COUNT = 19
 };
 #define FF_TIMING_MAX_RECORDS 16384
 ff_status ff_timing_enable(int32_t class_mask);

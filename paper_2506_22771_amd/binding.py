@@ -2,7 +2,7 @@
 
 Functions mirror the C-ABI names.  Tensor arguments are torch CUDA tensors (or None where the
 header allows NULL); their data_ptr() is handed to the library together with the current
-torch stream.  The layer norm and checkpoint calls take the compiled way (csrc/bind.cpp).  Nothing here computes."""
+torch stream.  The calls on matrices of floating-point values (norms, checkpoints, gated layers, dropout) take the compiled way (csrc/bind.cpp).  Nothing here computes."""
 from __future__ import annotations
 
 import ctypes as C
@@ -114,6 +114,20 @@ def lib() -> C.CDLL:
         L.ff_ckpt_weight_grad_workspace_bytes.argtypes = [i64, i64, i64]
         L.ff_ckpt_weight_grad.restype = i32
         L.ff_ckpt_weight_grad.argtypes = [P, i32, i64, P, P, i64, i64, i64, P, P, i32, P, P, i32, P, sz, P]
+        L.ff_gated_workspace_bytes.restype = sz
+        L.ff_gated_workspace_bytes.argtypes = [i64, i64, i64]
+        L.ff_gated_forward.restype = i32
+        L.ff_gated_forward.argtypes = [i64, i64, i64, P, P, P, P, i32, P, i32, i64, P, P, P, P, P, P, sz, P]
+        L.ff_gated_backward.restype = i32
+        L.ff_gated_backward.argtypes = [P, P, P, P, i64, i64, i32, P, P, i64, P, i64, P, i64, i32, P]
+        L.ff_group_norm_workspace_bytes.restype = sz
+        L.ff_group_norm_workspace_bytes.argtypes = [i64, i64, i64, i64]
+        L.ff_group_norm_forward.restype = i32
+        L.ff_group_norm_forward.argtypes = [i64, i64, i64, i64, i32, i32, P, i64, P, P, f32, i32, P, i64, P, P, P, P, P, i32, u64, u64, P, sz, P]
+        L.ff_group_norm_backward.restype = i32
+        L.ff_group_norm_backward.argtypes = [i64, i64, i64, i64, i32, i32, P, i64, P, P, i64, P, P, P, P, P, P, i32, P, i64, P, P, i32, P, sz, P]
+        L.ff_dropout.restype = i32
+        L.ff_dropout.argtypes = [i64, i64, i32, P, i64, P, i64, f32, u64, u64, P, P, i64, P]
         L.ff_timing_enable.restype = i32
         L.ff_timing_enable.argtypes = [i32]
         L.ff_timing_clock_probe.restype = i32
@@ -365,8 +379,43 @@ def ff_ckpt_weight_grad(dy, q, e, gamma, beta, dw, db, accumulate, ws) -> None:
     _chk(_native().ckpt_weight_grad(dy, q, e, gamma, beta, dw, db, accumulate, ws, _stream()), "ff_ckpt_weight_grad")
 
 
+# --- gated layers, group norm, dropout: tensors as above.  Maps are matrices [samples * pixels, channels].
+def ff_gated_workspace_bytes(rows: int, n: int, k: int) -> int:
+    return int(lib().ff_gated_workspace_bytes(rows, n, k))
+
+
+def ff_gated_forward(a_q, w_q, s_a, s_w, k, act, y, goodness, qg, eg, qu, eu, ws) -> None:
+    """a_q int8 [rows, ff_pitch(k)], w_q int8 [2n, ff_pitch(k)] with the gate's rows first, y [rows, n]."""
+    _chk(_native().gated_forward(a_q, w_q, s_a, s_w, k, act, y, goodness, qg, eg, qu, eu, ws, _stream()), "ff_gated_forward")
+
+
+def ff_gated_backward(qg, eg, qu, eu, act, coeff, dy, dg, du) -> None:
+    _chk(_native().gated_backward(qg, eg, qu, eu, act, coeff, dy, dg, du, _stream()), "ff_gated_backward")
+
+
+def ff_group_norm_workspace_bytes(samples: int, pixels: int, channels: int, groups: int) -> int:
+    return int(lib().ff_group_norm_workspace_bytes(samples, pixels, channels, groups))
+
+
+def ff_group_norm_forward(x, samples, groups, weight, bias, eps, act, y, mean, rstd, goodness, q, e, round_mode, seed, stream_tag, ws) -> None:
+    _chk(_native().group_norm_forward(x, samples, groups, weight, bias, eps, act, y, mean, rstd, goodness, q, e, round_mode, seed, stream_tag, ws,
+                                      _stream()), "ff_group_norm_forward")
+
+
+def ff_group_norm_backward(dy, coeff, x, mean, q, e, rstd, samples, groups, weight, bias, act, dx, dweight, dbias, accumulate, ws) -> None:
+    """h comes from x, mean and rstd, or, with x = None, from the checkpoint q, e and rstd."""
+    _chk(_native().group_norm_backward(dy, coeff, x, mean, q, e, rstd, samples, groups, weight, bias, act, dx, dweight, dbias, accumulate, ws, _stream()),
+         "ff_group_norm_backward")
+
+
+def ff_dropout(x, r, p, seed, stream_tag, step, y) -> None:
+    """step: an int64 tensor of one element that is read when the kernel runs, or None."""
+    _chk(_native().dropout(x, r, p, seed, stream_tag, step, y, _stream()), "ff_dropout")
+
+
 KERNEL_CLASSES = ("gemm_fwd", "gemm_dw", "quant_act", "quant_grad", "quant_w", "update", "absmax", "small", "im2col",
-                  "residual", "dwconv", "chain", "fused", "norm", "ckpt", "ckpt_dw")
+                  "residual", "dwconv", "chain", "fused", "norm", "ckpt", "ckpt_dw",
+                  "gated", "group_norm", "dropout")
 
 
 def ff_timing_enable(on, classes: Optional[Sequence[str]] = None) -> None:

@@ -1,0 +1,59 @@
+// Activation functions with their derivatives, for values of type T (what they are rounded to decides how close they are).
+#pragma once
+
+#include "ckpt.hpp"
+
+namespace ffi {
+
+// f(u) and f'(u).  GELU's exponential is the density's as well as a factor of Phi(-|u|).
+// 16-bit values: Phi(-|u|) = 1/2 t (a1 + t (a2 + ...)) exp(-u^2/2), t = 1 / (1 + p |u| / sqrt 2): Abramowitz and Stegun 7.1.26, off by at most 0.75e-7, far
+// below their rounding of 2^-9 or 2^-12.  With more arithmetic than this the large case is bound by it and not by memory: 16384 x 4096 bf16 values 96 us with
+// the library's erf and exp, 62 to 65 this way.
+// fp32 values: that is more than the rounding of an fp32 product (rms of f' 9.7e-8 of its size), so Phi = 1/2 + u P(u^2) up to |u| = 1.25, off by at most 2.1e-9, and
+// Phi(-|u|) = t Q(t) exp(-u^2/2), t = 1 / (1 + 0.3 |u|), beyond, off by at most 4.3e-9; P and Q are least-squares fits, reweighted towards the smallest largest
+// error (rms of f' 4.0e-8; with the device library's erf 4.1e-8, and 16384 x 4096 values with goodness 114 us, 120 that way, 109 by the sum above and with ReLU).
+// ANY: of any fp32 argument; else of what a checkpoint holds.
+template <typename T, int ACT, bool ANY = false> __device__ __forceinline__ void act_of(float u, float& f, float& d)
+{
+    if constexpr (ACT == FF_ACT_RELU) {
+        f = u > 0 ? u : (u == u ? 0.0f : u);
+        d = u > 0 ? 1.0f : (u == u ? 0.0f : u);
+    } else if constexpr (ACT == FF_ACT_GELU) {
+        const float e = __builtin_amdgcn_exp2f(u * u * -0.72134752044448170f);              // exp(-u^2 / 2)
+        float phi;
+        if constexpr (sizeof(T) == 4) {
+            const float s = u * u, t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(u), 0.3f, 1.0f));
+            float p = __builtin_fmaf(s, -6.64486e-6f, 1.1032746e-4f);
+            p = __builtin_fmaf(s, p, -1.1827096e-3f);
+            p = __builtin_fmaf(s, p, 9.9715004e-3f);
+            p = __builtin_fmaf(s, p, -0.06648999f);
+            p = __builtin_fmaf(s, p, 0.39894226f);
+            float q = __builtin_fmaf(t, -0.033505592f, 0.30637836f);
+            q = __builtin_fmaf(t, q, -0.06527595f);
+            q = __builtin_fmaf(t, q, 0.18152371f);
+            q = __builtin_fmaf(t, q, 0.11132239f);
+            const float low = t * q * e;
+            phi = __builtin_fabsf(u) < 1.25f ? __builtin_fmaf(u, p, 0.5f) : u > 0 ? 1.0f - low : low;
+        } else {
+            const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(u), 0.23164189110f, 1.0f));   // p / sqrt 2
+            float q = __builtin_fmaf(t, 0.5307027145f, -0.7265760135f);                     // half of the polynomial
+            q = __builtin_fmaf(t, q, 0.7107068705f);
+            q = __builtin_fmaf(t, q, -0.142248368f);
+            q = __builtin_fmaf(t, q, 0.127414796f);
+            // Phi(u): 1 - low above zero, else low; a code that is not zero stands for 2^-106 at least
+            if constexpr (ANY) phi = u > 0 ? 1.0f - t * q * e : t * q * e;
+            else phi = __builtin_fabsf(__builtin_amdgcn_fmed3f(u * 0x1p127f, 0.0f, 1.0f) - t * q * e);
+        }
+        f = u * phi;
+        d = __builtin_fmaf(u * e, 0.39894228040143268f, phi);
+    } else if constexpr (ACT == FF_ACT_SILU) {
+        const float sig = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * -1.4426950408889634f));
+        f = u * sig;
+        d = __builtin_fmaf(f, 1.0f - sig, sig);
+    } else {
+        f = u;
+        d = 1.0f;
+    }
+}
+
+}  // namespace ffi

@@ -1,4 +1,4 @@
-// Python's side of the layer norm and checkpoint calls: shapes, types, strides and devices of the tensors are compared here (all lie on the current
+// Python's side of the calls on matrices of floating-point values (norms, checkpoints, gated layers, dropout): shapes, types, strides and devices of the tensors are compared here (all lie on the current
 // device, whose stream the work goes to) and their addresses handed to the library.  Marshalling only, in C++ because these calls are short: a norm of one 4096-wide row took 8.3 us through
 // ctypes, nearly all of it spent on attributes and argument conversions in Python.
 //
@@ -142,6 +142,38 @@ Ckpt checkpoint(PyObject* q, PyObject* e, int64_t rows, int64_t cols)
     return c;
 }
 
+// An int8 matrix as the library's quantiser writes it.
+const void* codes(PyObject* o, const char* what, int64_t rows, int64_t pitch)
+{
+    const at::Tensor& t = tensor(o, what);
+    if (t.scalar_type() != at::kChar || t.dim() != 2 || t.size(0) != rows || t.size(1) != pitch || !t.is_contiguous()) refuse(what, "contiguous int8", rows, pitch);
+    on_device(t, what);
+    return t.data_ptr();
+}
+const float* scalar(PyObject* o, const char* what)
+{
+    const at::Tensor& t = tensor(o, what);
+    if (t.scalar_type() != at::kFloat || t.numel() != 1) refuse(what, "one float32");
+    on_device(t, what);
+    return (const float*)t.data_ptr();
+}
+float* table(PyObject* o, const char* what, int64_t rows, int64_t cols)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = tensor(o, what);
+    if (t.scalar_type() != at::kFloat || t.dim() != 2 || t.size(0) != rows || t.size(1) != cols || !t.is_contiguous()) refuse(what, "contiguous float32", rows, cols);
+    on_device(t, what);
+    return (float*)t.data_ptr();
+}
+const uint64_t* step(PyObject* o)   // a step number in device memory
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = tensor(o, "step");
+    if (t.scalar_type() != at::kLong || t.numel() != 1) refuse("step", "one int64");
+    on_device(t, "step");
+    return (const uint64_t*)t.data_ptr();
+}
+
 struct Bytes {
     void* p = nullptr;
     size_t n = 0;
@@ -273,9 +305,82 @@ PyObject* ckpt_weight_grad(PyObject*, PyObject* const* args, Py_ssize_t n)
     });
 }
 
+PyObject* gated_forward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return call<14>(args, n, [](PyObject* const* a) {
+        const Mat y = matrix(a[6], "y");
+        const int64_t k = whole(a[4]), pitch = ff_pitch(k);
+        const void *aq = codes(a[0], "a_q", y.rows, pitch), *wq = codes(a[1], "w_q", 2 * y.cols, pitch);
+        const Ckpt g = checkpoint(a[8], a[9], y.rows, y.cols), u = checkpoint(a[10], a[11], y.rows, y.cols);
+        const Bytes ws = workspace(a[12]);
+        return ff_gated_forward(y.rows, y.cols, k, (const int8_t*)aq, (const int8_t*)wq, scalar(a[2], "s_a"), scalar(a[3], "s_w"), small(a[5]), y.p, y.kind, y.ld,
+                                floats(a[7], "goodness", y.rows), g.q, g.e, u.q, u.e, ws.p, ws.n, address(a[13]));
+    });
+}
+
+PyObject* gated_backward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return call<10>(args, n, [](PyObject* const* a) {
+        const Mat dg = matrix(a[7], "dg"), du = matrix_like(a[8], "du", dg), dy = maybe_matrix_like(a[6], "dy", dg);
+        const Ckpt g = checkpoint(a[0], a[1], dg.rows, dg.cols), u = checkpoint(a[2], a[3], dg.rows, dg.cols);
+        return ff_gated_backward(g.q, g.e, u.q, u.e, dg.rows, dg.cols, small(a[4]), floats(a[5], "coeff", dg.rows), dy.p, dy.ld, dg.p, dg.ld, du.p, du.ld, dg.kind,
+                                 address(a[9]));
+    });
+}
+
+// Pixels of a sample, of a map of so many rows.
+int64_t pixels_of(int64_t rows, int64_t samples, int64_t least = 1)
+{
+    if (samples < 0 || (samples == 0 ? rows != 0 : rows % samples != 0)) {
+        PyErr_Format(PyExc_ValueError, "samples: a number of equal parts of %lld rows expected", (long long)rows);
+        throw Refused();
+    }
+    return samples == 0 ? least : rows / samples;
+}
+
+PyObject* group_norm_forward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return call<18>(args, n, [](PyObject* const* a) {
+        const Mat x = matrix(a[0], "x"), y = matrix_like(a[7], "y", x);
+        const int64_t samples = whole(a[1]), groups = whole(a[2]), pixels = pixels_of(x.rows, samples);
+        const Params p = params(a[3], a[4], "weight", "bias", x.cols, x.type);
+        const Ckpt c = checkpoint(a[11], a[12], x.rows, x.cols);
+        const Bytes ws = workspace(a[16]);
+        return ff_group_norm_forward(samples, pixels, x.cols, groups, x.kind, p.kind, x.p, x.ld, p.a, p.b, real(a[5]), small(a[6]), y.p, y.ld,
+                                     table(a[8], "mean", samples, groups), table(a[9], "rstd", samples, groups), floats(a[10], "goodness", samples), c.q, c.e,
+                                     small(a[13]), word(a[14]), word(a[15]), ws.p, ws.n, address(a[17]));
+    });
+}
+
+PyObject* group_norm_backward(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return call<18>(args, n, [](PyObject* const* a) {
+        PyObject* const first = a[0] != Py_None ? a[0] : a[2] != Py_None ? a[2] : a[12];   // dy, x or dx
+        if (first == Py_None) refuse("dy, x or dx", "a matrix");
+        const Mat like = matrix(first, a[0] != Py_None ? "dy" : a[2] != Py_None ? "x" : "dx");
+        const Mat dy = maybe_matrix_like(a[0], "dy", like), x = maybe_matrix_like(a[2], "x", like), dx = maybe_matrix_like(a[12], "dx", like);
+        const int64_t samples = whole(a[7]), groups = whole(a[8]), pixels = pixels_of(like.rows, samples);
+        const Ckpt c = checkpoint(a[4], a[5], like.rows, like.cols);
+        const Params p = params(a[9], a[10], "weight", "bias", like.cols, like.type);
+        const Bytes ws = workspace(a[16]);
+        return ff_group_norm_backward(samples, pixels, like.cols, groups, like.kind, p.kind, dy.p, dy.ld, floats(a[1], "coeff", samples), x.p, x.ld,
+                                      table(a[3], "mean", samples, groups), c.q, c.e, table(a[6], "rstd", samples, groups), p.a, p.b, small(a[11]), dx.p, dx.ld,
+                                      floats(a[13], "dweight", like.cols), floats(a[14], "dbias", like.cols), truth(a[15]), ws.p, ws.n, address(a[17]));
+    });
+}
+
+PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    return call<8>(args, n, [](PyObject* const* a) {
+        const Mat x = matrix(a[0], "x"), r = maybe_matrix_like(a[1], "r", x), y = matrix_like(a[6], "y", x);
+        return ff_dropout(x.rows, x.cols, x.kind, x.p, x.ld, r.p, r.ld, real(a[2]), word(a[3]), word(a[4]), step(a[5]), y.p, y.ld, address(a[7]));
+    });
+}
+
 #define METHOD(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(layer_norm_forward), METHOD(layer_norm_backward), METHOD(ckpt_store), METHOD(ckpt_load),
-                         METHOD(ckpt_act_backward),  METHOD(ckpt_weight_grad),    {nullptr, nullptr, 0, nullptr}};
+                         METHOD(ckpt_act_backward),  METHOD(ckpt_weight_grad),    METHOD(gated_forward),
+                         METHOD(gated_backward),     METHOD(group_norm_forward),  METHOD(group_norm_backward), METHOD(dropout), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

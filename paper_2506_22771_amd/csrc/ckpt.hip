@@ -8,39 +8,11 @@
 // arithmetic: 25 operations a value), load 38 (5.3), ReLU backward 59 (5.7), GELU 64 (5.3); fp32 60 (5.6), 63 (5.3), 69 (4.9), 108 (5.6), 114 (5.3).
 // All three are bound by memory but for that.  A lane has eight columns (a chunk) of a row, a quad of lanes one block; a workgroup takes consecutive chunks,
 // whatever the row length, and has all its loads in flight before the first is used.
-#include <type_traits>
-
-#include "ckpt.hpp"
+#include "act.hpp"
+#include "chunks.hpp"
 #include "norm.hpp"
 
 namespace ffi {
-
-constexpr int CK_THREADS = 256;
-
-// Consecutive chunks of a matrix; rows are `slots` chunks long (a multiple of four, so that quads hold blocks).
-struct Chunks {
-    int64_t total;
-    uint32_t slots, magic;   // magic: ceil(2^32 / slots)
-};
-static Chunks chunks_of(int64_t rows, int64_t bytes_or_cols)
-{
-    const int64_t slots = (bytes_or_cols + 31) / 32 * 4;
-    return {rows * slots, (uint32_t)slots, (uint32_t)(((uint64_t(1) << 32) + (uint64_t)slots - 1) / (uint64_t)slots)};
-}
-// Row (from the workgroup's first one, row0, on) and chunk of `at` chunks (fewer than 4096) behind the workgroup's first one, (row0, chunk0).  Rows of 4096
-// chunks or more: at most one row further; shorter ones: at + chunk0 < 8192, where the product with the rounded-up reciprocal has the quotient exactly.
-__device__ __forceinline__ void chunk_place(const Chunks& c, uint32_t chunk0, uint32_t at, uint32_t& r, uint32_t& chunk)
-{
-    const uint32_t o = chunk0 + at;
-    r = c.slots >= 4096u ? (o >= c.slots ? 1u : 0u) : __umulhi(o, c.magic);
-    chunk = o - r * c.slots;
-}
-__device__ __forceinline__ void chunk_first(const Chunks& c, int64_t first, int64_t& row0, uint32_t& chunk0)
-{
-    const uint32_t r = (uint32_t)first / c.slots;   // (a matrix has fewer than 2^31 chunks: size_status)
-    row0 = r;
-    chunk0 = (uint32_t)first - r * c.slots;
-}
 
 template <typename T> struct CkptArgs {
     Chunks c;
@@ -52,17 +24,6 @@ template <typename T> struct CkptArgs {
     const float* coeff;   // act backward: may be null
     int32_t cols, act;
 };
-
-// A chunk `at` chunks behind the workgroup's first one: its place (the workgroup's first row's first chunk where there is none) and how many of its columns
-// exist.
-__device__ __forceinline__ int chunk_at(const Chunks& c, int cols, int64_t first, uint32_t chunk0, uint32_t at, uint32_t& r, uint32_t& chunk)
-{
-    chunk_place(c, chunk0, at, r, chunk);
-    const bool there = first + at < c.total;
-    r = there ? r : 0;
-    chunk = there ? chunk : 0;
-    return there ? max(0, min(8, cols - 8 * (int)chunk)) : 0;
-}
 
 template <typename T, RowEnds ENDS, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckpt_store(CkptArgs<T> a)
 {
@@ -128,55 +89,6 @@ template <typename T, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckp
     }
 }
 
-// f(u) and f'(u).  GELU's exponential is the density's as well as a factor of Phi(-|u|).
-// 16-bit values: Phi(-|u|) = 1/2 t (a1 + t (a2 + ...)) exp(-u^2/2), t = 1 / (1 + p |u| / sqrt 2): Abramowitz and Stegun 7.1.26, off by at most 0.75e-7, far
-// below their rounding of 2^-9 or 2^-12.  With more arithmetic than this the large case is bound by it and not by memory: 16384 x 4096 bf16 values 96 us with
-// the library's erf and exp, 62 to 65 this way.
-// fp32 values: that is more than the rounding of an fp32 product (rms of f' 9.7e-8 of its size), so Phi = 1/2 + u P(u^2) up to |u| = 1.25, off by at most 2.1e-9, and
-// Phi(-|u|) = t Q(t) exp(-u^2/2), t = 1 / (1 + 0.3 |u|), beyond, off by at most 4.3e-9; P and Q are least-squares fits, reweighted towards the smallest largest
-// error (rms of f' 4.0e-8; with the device library's erf 4.1e-8, and 16384 x 4096 values with goodness 114 us, 120 that way, 109 by the sum above and with ReLU).
-template <typename T, int ACT> __device__ __forceinline__ void act_of(float u, float& f, float& d)
-{
-    if constexpr (ACT == FF_ACT_RELU) {
-        f = u > 0 ? u : (u == u ? 0.0f : u);
-        d = u > 0 ? 1.0f : (u == u ? 0.0f : u);
-    } else if constexpr (ACT == FF_ACT_GELU) {
-        const float e = __builtin_amdgcn_exp2f(u * u * -0.72134752044448170f);              // exp(-u^2 / 2)
-        float phi;
-        if constexpr (sizeof(T) == 4) {
-            const float s = u * u, t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(u), 0.3f, 1.0f));
-            float p = __builtin_fmaf(s, -6.64486e-6f, 1.1032746e-4f);
-            p = __builtin_fmaf(s, p, -1.1827096e-3f);
-            p = __builtin_fmaf(s, p, 9.9715004e-3f);
-            p = __builtin_fmaf(s, p, -0.06648999f);
-            p = __builtin_fmaf(s, p, 0.39894226f);
-            float q = __builtin_fmaf(t, -0.033505592f, 0.30637836f);
-            q = __builtin_fmaf(t, q, -0.06527595f);
-            q = __builtin_fmaf(t, q, 0.18152371f);
-            q = __builtin_fmaf(t, q, 0.11132239f);
-            const float low = t * q * e;
-            phi = __builtin_fabsf(u) < 1.25f ? __builtin_fmaf(u, p, 0.5f) : u > 0 ? 1.0f - low : low;
-        } else {
-            const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(u), 0.23164189110f, 1.0f));   // p / sqrt 2
-            float q = __builtin_fmaf(t, 0.5307027145f, -0.7265760135f);                     // half of the polynomial
-            q = __builtin_fmaf(t, q, 0.7107068705f);
-            q = __builtin_fmaf(t, q, -0.142248368f);
-            q = __builtin_fmaf(t, q, 0.127414796f);
-            // Phi(u): 1 - low above zero, else low; a code that is not zero stands for 2^-106 at least
-            phi = __builtin_fabsf(__builtin_amdgcn_fmed3f(u * 0x1p127f, 0.0f, 1.0f) - t * q * e);
-        }
-        f = u * phi;
-        d = __builtin_fmaf(u * e, 0.39894228040143268f, phi);
-    } else if constexpr (ACT == FF_ACT_SILU) {
-        const float sig = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * -1.4426950408889634f));
-        f = u * sig;
-        d = __builtin_fmaf(f, 1.0f - sig, sig);
-    } else {
-        f = u;
-        d = 1.0f;
-    }
-}
-
 template <typename T, int ACT, RowEnds ENDS, int U> __global__ __launch_bounds__(CK_THREADS) void k_ckpt_act_backward(CkptArgs<T> a)
 {
     const int64_t first = (int64_t)blockIdx.x * (CK_THREADS * U);
@@ -234,14 +146,6 @@ template <typename T> static CkptArgs<T> ckpt_args(const int8_t* q, const uint8_
     a.cols = (int32_t)cols;
     return a;
 }
-template <typename F> static void by_ends(int64_t cols, bool in_place, F&& launch)
-{
-    if (cols % 8 == 0) launch(std::integral_constant<RowEnds, ROWS_WHOLE>());
-    else if (cols > 8 && !in_place) launch(std::integral_constant<RowEnds, ROWS_RAGGED>());
-    else launch(std::integral_constant<RowEnds, ROWS_OWN>());
-}
-template <int U> static unsigned ckpt_grid(const Chunks& c) { return (unsigned)((c.total + CK_THREADS * U - 1) / (CK_THREADS * U)); }
-
 template <typename T> static hipError_t store_of(const void* x, int64_t ldx, int64_t rows, int64_t cols, const CkptRound& r, int8_t* q, uint8_t* e, hipStream_t s)
 {
     CkptArgs<T> a = ckpt_args<T>(q, e, rows, cols, pitch8(cols));   // pad columns are written too

@@ -1,0 +1,122 @@
+// How the group norm's launches cut up their maps (group_norm.hip).  Host code alone, so that it can be built and asked without the kernels.
+//
+// A workgroup's threads lie over a slab: `slots` chunks of eight columns wide and `lanes` pixels high, a thread keeping its chunk's columns from pixel to pixel.
+#pragma once
+
+#include <algorithm>
+#include <cstddef>
+#include <cstdint>
+
+namespace ffi {
+
+constexpr int GN_SPLIT_THREADS = 256;
+constexpr int GN_APPLY_ROWS = 4;      // pixels of a thread of the launches that apply what others have summed
+constexpr int GN_MOST_GRID = 1 << 20; // workgroups of a launch; they take item after item
+constexpr size_t GN_MOST_LDS = 150 * 1024;
+
+struct GnCut {
+    int32_t threads, slots, lanes;   // of a workgroup
+    int32_t slice, slices;           // columns of a slice, slices of a row
+};
+// Sums of a chunk that are kept apart: one where every chunk lies in one group, two where its halves do, else eight; of columns always eight.
+static int gn_cells(int64_t d, bool backward) { return backward ? 8 : d % 8 == 0 ? 1 : d % 4 == 0 ? 2 : 8; }
+// threads that share the sum of a cell over the lanes, at most
+static int gn_parts(int threads, int64_t slots, int cells) { return (int)std::max<int64_t>(1, std::min<int64_t>(16, std::min<int64_t>(threads / slots, threads / (slots * cells)))); }
+// LDS of a workgroup: sums of two values per cell, of groups, and a row of weights
+static size_t gn_lds(int threads, int64_t slots, int cells, int64_t d)
+{
+    return sizeof(float) * (size_t)(2 * slots * cells * (1 + gn_parts(threads, slots, cells) + threads / slots) + 2 * ((slots * 8 + d - 1) / d + 1) + 8 * slots);
+}
+struct GnPlan {
+    bool whole;          // a workgroup holds whole groups in registers: one launch
+    GnCut cut;           // whole: slices of whole groups.  Else those of the launches that apply
+    GnCut stat;          // else: slices of the statistics' launch, of whole groups or of pieces of one
+    int32_t pieces;      // slices of one group (1: a slice has whole groups)
+    int32_t blocks;      // stat: workgroups of a slice over the pixels
+    int32_t apply_blocks;
+};
+
+constexpr int64_t gn_gcd(int64_t a, int64_t b) { return b == 0 ? a : gn_gcd(b, a % b); }
+static int64_t gn_up(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
+
+// rows of a thread of the launch that holds its slab in registers
+static int gn_rows(int size, bool backward) { return size == 4 ? (backward ? 2 : 4) : (backward ? 4 : 8); }
+
+// size: bytes of an element; kept: a checkpoint is written or read, whose blocks of 32 columns lie in one workgroup; span: columns a row has to be covered to
+static GnPlan gn_plan(int64_t samples, int64_t pixels, int64_t channels, int64_t groups, int size, bool kept, int64_t span, bool backward)
+{
+    GnPlan p = {};
+    const int64_t d = channels / groups, unit = kept ? 32 : 8, step = d / gn_gcd(d, unit) * unit;
+    const int64_t row = gn_up(kept ? span : channels, unit);   // columns of a row with what is behind it
+    const int rows = gn_rows(size, backward);
+    // Slices from the narrowest on: as wide as 128 bytes, then wider while there are workgroups to spare and threads without a pixel, or none that fit.
+    for (int threads : {256, 1024}) {
+        int64_t best = 0;
+        for (int64_t w = std::min(step, row);; w = std::min(w + step, row)) {
+            const int64_t slots = (w + 7) / 8;
+            if (slots > threads || gn_lds(threads, slots, gn_cells(d, backward), d) > GN_MOST_LDS) break;
+            const int64_t lanes = threads / slots, slices = (row + w - 1) / w;
+            if ((pixels + lanes - 1) / lanes > rows) break;
+            best = w;
+            if (w >= row) break;
+            const bool narrow = w * size < 128, idle = pixels * slots < 2 * threads && samples * slices > 1024;
+            if (!narrow && !idle) break;
+        }
+        if (best == 0) continue;
+        if (threads == 256 && best < row && best * size < 128) {   // wider lines in larger workgroups, where they hold them
+            const int64_t w = std::min(gn_up(128 / size, step), row), slots = (w + 7) / 8;
+            if (slots <= 1024 && gn_lds(1024, slots, gn_cells(d, backward), d) <= GN_MOST_LDS && (pixels + 1024 / slots - 1) / (1024 / slots) <= rows) continue;
+        }
+        const int32_t slots = (int32_t)((best + 7) / 8);
+        p.whole = true;
+        p.cut = {threads, slots, threads / slots, (int32_t)best, (int32_t)((row + best - 1) / best)};
+        return p;
+    }
+    // Statistics by slices of about 128 bytes, of whole groups or of an equal piece of one.
+    const int64_t wide = std::max<int64_t>(8, 128 / size);
+    int64_t w;
+    p.pieces = 1;
+    if (d <= wide) {
+        w = wide / d * d;
+        p.stat.slices = (int32_t)((channels + w - 1) / w);
+    } else {
+        const int64_t pieces = (d + wide - 1) / wide;
+        w = gn_up((d + pieces - 1) / pieces, 8);
+        p.pieces = (int32_t)((d + w - 1) / w);
+        p.stat.slices = (int32_t)(groups * p.pieces);
+    }
+    p.stat.threads = GN_SPLIT_THREADS;
+    p.stat.slice = (int32_t)w;
+    p.stat.slots = (int32_t)((w + 7) / 8);
+    p.stat.lanes = GN_SPLIT_THREADS / p.stat.slots;
+    const int64_t slots = std::min<int64_t>(gn_up(row, unit) / 8, std::max<int64_t>(unit / 8, 128 / size / 8));
+    p.cut.threads = GN_SPLIT_THREADS;
+    p.cut.slots = (int32_t)slots;
+    p.cut.lanes = (int32_t)(GN_SPLIT_THREADS / slots);
+    p.cut.slice = (int32_t)(slots * 8);
+    p.cut.slices = (int32_t)((row + p.cut.slice - 1) / p.cut.slice);
+    p.apply_blocks = (int32_t)((pixels + (int64_t)p.cut.lanes * GN_APPLY_ROWS - 1) / ((int64_t)p.cut.lanes * GN_APPLY_ROWS));
+    if (!backward) {
+        p.blocks = (int32_t)((pixels + (int64_t)p.stat.lanes * rows - 1) / ((int64_t)p.stat.lanes * rows));
+    } else {
+        // sums of columns, whatever group they are of: the slices that apply, over as many blocks of pixels as keep every compute unit busy
+        p.stat = p.cut;
+        p.pieces = 1;
+        const int64_t most = (pixels + p.cut.lanes - 1) / p.cut.lanes, want = (2048 + samples * p.cut.slices - 1) / (samples * p.cut.slices);
+        p.blocks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(most, want), 128));
+    }
+    return p;
+}
+
+// floats of workspace
+static size_t gn_forward_floats(const GnPlan& p, int64_t samples, int64_t groups)
+{
+    if (p.whole) return (size_t)(samples * p.cut.slices);
+    return (size_t)(4 * samples * groups * p.pieces * p.blocks + 4 * samples * groups + samples * p.cut.slices * p.apply_blocks);
+}
+static size_t gn_backward_floats(const GnPlan& p, int64_t samples, int64_t channels, int64_t groups)
+{
+    return (size_t)(2 * samples * channels + (p.whole ? 0 : 2 * samples * channels * p.blocks + 2 * samples * groups));
+}
+
+}  // namespace ffi
