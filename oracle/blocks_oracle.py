@@ -8,7 +8,7 @@ from .norm_oracle import act, uniforms
 
 def gated_forward(a_q, w_q, scale, kind):
     """(y, goodness, g, u) in fp64 from int8 codes without pad columns; w_q [2n, k], the gate's rows first."""
-    acc = a_q.astype(np.int64) @ w_q.astype(np.int64).T
+    acc = a_q.astype(np.float64) @ w_q.astype(np.float64).T    # (whole numbers below 2^53: exact)
     n = w_q.shape[0] // 2
     g, u = acc[:, :n] * float(scale), acc[:, n:] * float(scale)
     y = act(kind, g)[0] * u

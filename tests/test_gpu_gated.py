@@ -98,6 +98,36 @@ def test_forward_of_every_type(rows, n, k, dtype):
     check_kept(*ku, u, du)
 
 
+# tiles of 128 x 64 and of 256 x 128 outputs, one and several to a workgroup, reductions of one step to several, at both sides of a tile's end
+MANY = [(2000, 1500, 90, "float32"), (8200, 2050, 260, "float16"), (8200, 2050, 100, "bfloat16"), (3000, 1500, 130, "float16"), (8150, 2040, 90, "bfloat16"),
+        (8192, 2048, 500, "float32"), (70000, 120, 128, "bfloat16"), (40, 32767, 40, "float32")]
+
+
+@pytest.mark.parametrize("rows, n, k, dtype", MANY)
+def test_forward_of_many_tiles(rows, n, k, dtype):
+    """Against 64 bits on the device."""
+    a, w, s_a, s_w = layer(rows, n, k)
+    gy, ggood, kg, ku = run_forward(a, w, s_a, s_w, "silu", dtype, left=3, right=2)
+    scale = float(s_a) * float(s_w)
+    acc = [torch.from_numpy(a).cuda().double() @ torch.from_numpy(p).cuda().double().t() for p in (w[:n], w[n:])]
+    g, u = acc[0] * scale, acc[1] * scale
+    sig = torch.sigmoid(g)
+    y = g * sig * u
+    f = (g * sig).abs()
+    # as forward_bounds has it
+    dy = (16 * U * (f + 0.2 * g.abs()) + 1.13 * 3 * U * g.abs()) * u.abs() + f * 3 * U * u.abs() + 2 * U * y.abs()
+    assert ((gy.double() - y).abs() <= dy * (1 + HALF_ULP[dtype]) + y.abs() * HALF_ULP[dtype] + TINY[dtype]).all()
+    assert ((ggood.double() - (y * y).sum(1)).abs() <= (2 * y.abs() * dy + dy**2).sum(1) + (66 + n // 32) * U * (y * y).sum(1)).all()
+    for (q, e), v in ((kg, g), (ku, u)):
+        nb = (n + 31) // 32
+        assert not q[:, n:].any() and not e[:, nb:].any()
+        step = torch.exp2(e[:, :nb].double() - 127).repeat_interleave(32, 1)[:, :n]
+        assert ((q[:, :n].double() * step - v).abs() <= 3 * U * v.abs() + 0.5 * step).all()
+        top = torch.nn.functional.pad(v.abs(), (0, nb * 32 - n)).view(rows, nb, 32).amax(2)
+        span = 127 * torch.exp2(e[:, :nb].double() - 127)       # the smallest power of two that covers the block
+        assert (top <= span * (1 + 4 * U)).all() and (top * (1 + 4 * U) > span / 2).all()
+
+
 @pytest.mark.parametrize("rows", [3, 300])
 def test_largest_sums_and_extreme_scales(rows):
     """Sums at the end of int32 (all codes alike, the longest reduction), zero codes, and scales that leave fp32's range."""
