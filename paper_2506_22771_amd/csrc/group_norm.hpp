@@ -1,0 +1,219 @@
+// Group norm with an activation over channels-last maps, forward and backward.
+//
+//   per sample and group, over its d channels at all P pixels:  mean, rstd = 1 / sqrt(1/(P d) sum (x - mean)^2 + eps),  h = (x - mean) rstd
+//   z = h gamma + beta,  y = f(z),  G = sum over the sample of f(z)^2
+//   dz = (dy + 2 c f(z)) f'(z),  dgamma = sum over pixels and samples of dz h,  dbeta = sum of dz
+//   dx = rstd (g - 1/(P d) sum over the group of g - h 1/(P d) sum over the group of g h),  g = gamma dz
+//
+// Statistics, products and sums are fp32 (the means of parts of a group are joined in 64 bits); y and dx are rounded once.  As in the layer norm, the mean of
+// the deviations is taken out of groups farther from zero than they are wide (norm_math.hpp).
+//
+// Memory bounds all of it.  A workgroup's threads lie over a slab of whole groups: a chunk of eight columns is a thread's own from pixel to pixel, so that
+// parameters and sums of columns stay in registers, and sums meet in LDS once.  Where such a slab fits the registers of a workgroup, everything is read once
+// (one launch, `whole` below; group_norm_plan.hpp).  Else a first launch sums parts of groups, a small one joins them, and a third reads again and applies.
+// The sums of all samples, dgamma and dbeta, are a launch of their own over sums of columns per sample.
+#pragma once
+
+#include "act.hpp"
+#include "blocks.hpp"
+#include "group_norm_plan.hpp"
+#include "norm_math.hpp"
+
+namespace ffi {
+
+// ---- slabs ------------------------------------------------------------------------------------------------------------
+struct Slab {
+    int32_t slots, lanes, slice, slices;   // see GnCut
+    int32_t pixels, channels, groups, d;
+    int32_t parts;             // threads that share the sum of a cell over the lanes, at most
+    int64_t items, per_xcd;    // workgroups' work: (sample, [block of pixels,] slice)
+};
+// Items in turn to the eight XCDs, so that neighbours, which share cache lines, meet in one L2; -1: none.
+__device__ __forceinline__ int64_t item_of(const Slab& s, int64_t turn)
+{
+    const int64_t i = (turn & 7) * s.per_xcd + (turn >> 3);
+    return i < s.items ? i : -1;
+}
+
+// A thread's place in its slab.  Not to be traced back: the compiler would work out all that follows from it ahead of the loop over items, and keep it.
+__device__ __forceinline__ void place_of(const Slab& s, int& c, int& pl)
+{
+    uint32_t t = threadIdx.x;
+    opaque(t);
+    c = t % (uint32_t)s.slots;
+    pl = t / (uint32_t)s.slots;
+}
+
+// What the compiler is not to mix with what follows: several pixels' values at once take more registers than there are.
+__device__ __forceinline__ void one_pixel_at_a_time() { __builtin_amdgcn_sched_barrier(0); }
+
+__device__ __forceinline__ float wave_sum(float v)
+{
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+// What a thread keeps apart of its chunk: the halves (CELLS 2), where every group is a multiple of four channels, or every column (8).
+template <int CELLS> constexpr int cell_of(int column) { return CELLS == 2 ? column >> 2 : column; }
+// Every cell's group, counted from the slice's first column on, and its first column's place in it.
+template <int CELLS, typename F> __device__ __forceinline__ void of_cells(int first, int d, int groups, F&& each)
+{
+    if constexpr (CELLS == 2) {
+        const int g0 = first / d, g1 = (first + 4) / d;
+        each(0, min(g0, groups - 1), first - g0 * d);
+        each(1, min(g1, groups - 1), first + 4 - g1 * d);
+    } else {
+        int g = first / d, at = first - g * d;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            each(i, min(g, groups - 1), at);
+            if (++at == d) {
+                at = 0;
+                ++g;
+            }
+        }
+    }
+}
+
+// Sums over the lanes of K values of every cell, into lds[k * cells + i], cell i of the slots * CELLS.  lds: K cells (1 + parts + lanes) floats.  A barrier ends it.
+template <int K, int CELLS>
+__device__ __forceinline__ void sum_cells(const float (&v)[K][CELLS], int slots, int lanes, int most_parts, int c, int pl, float* lds)
+{
+    const int cells = slots * CELLS, parts = max(1, min(most_parts, (int)blockDim.x / (K * cells)));
+    float* const all = lds + K * cells * (1 + most_parts);
+    if (pl < lanes) {
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int i = 0; i < CELLS; ++i) all[(k * lanes + pl) * cells + c * CELLS + i] = v[k][i];
+    }
+    __syncthreads();
+    float* const some = lds + K * cells;
+    for (int t = threadIdx.x; t < K * cells * parts; t += (int)blockDim.x) {
+        const int part = t / (K * cells), kc = t - part * (K * cells), k = kc >= cells && K > 1 ? kc / cells : 0, i = kc - k * cells;
+        float s = 0;
+#pragma unroll 4
+        for (int l = part; l < lanes; l += parts) s += all[(k * lanes + l) * cells + i];
+        some[t] = s;
+    }
+    __syncthreads();
+    for (int t = threadIdx.x; t < K * cells; t += (int)blockDim.x) {
+        float s = 0;
+#pragma unroll 4
+        for (int part = 0; part < parts; ++part) s += some[part * (K * cells) + t];
+        lds[t] = s;
+    }
+    __syncthreads();
+}
+// Sums over the `n` cells of each of `groups` groups, by value(k, cell), into out[k * groups + g].  A barrier ends it.
+template <int K, typename F> __device__ __forceinline__ void sum_groups(int groups, int n, float* out, F&& value)
+{
+    if (n <= 16) {
+        for (int t = threadIdx.x; t < K * groups; t += (int)blockDim.x) {
+            const int k = K > 1 ? t / groups : 0, g = t - k * groups;
+            float s = 0;
+            for (int i = 0; i < n; ++i) s += value(k, g * n + i);
+            out[t] = s;
+        }
+    } else {
+        for (int t = threadIdx.x >> 6; t < K * groups; t += (int)blockDim.x / 64) {
+            const int k = K > 1 ? t / groups : 0, g = t - k * groups;
+            float s = 0;
+            for (int i = threadIdx.x & 63; i < n; i += 64) s += value(k, g * n + i);
+            s = wave_sum(s);
+            if ((threadIdx.x & 63) == 0) out[t] = s;
+        }
+    }
+    __syncthreads();
+}
+
+// Sum of a workgroup's values, in thread 0.  red: a word per wavefront.  A barrier begins it.
+__device__ __forceinline__ float sum_block(float v, float* red)
+{
+    v = wave_sum(v);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float s = 0;
+    if (threadIdx.x == 0)
+        for (int w = 0; w < (int)blockDim.x / 64; ++w) s += red[w];
+    return s;
+}
+
+template <typename T> __device__ __forceinline__ void activate(int act, const float z[8], float f[8])
+{
+    float d;
+    switch (act) {   // (uniform)
+        case FF_ACT_RELU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                act_of<T, FF_ACT_RELU, true>(z[i], f[i], d);
+                if (i & 1) one_pixel_at_a_time();
+            }
+            break;
+        case FF_ACT_GELU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                act_of<T, FF_ACT_GELU, true>(z[i], f[i], d);
+                if (i & 1) one_pixel_at_a_time();
+            }
+            break;
+        case FF_ACT_SILU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                act_of<T, FF_ACT_SILU, true>(z[i], f[i], d);
+                if (i & 1) one_pixel_at_a_time();
+            }
+            break;
+        default:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = z[i];
+    }
+}
+
+// ---- launches ----------------------------------------------------------------------------------------------------
+static Slab slab_of(const GnCut& c, int64_t samples, int64_t pixels, int64_t channels, int64_t groups, int64_t blocks, int cells)
+{
+    Slab s = {};
+    s.slots = c.slots;
+    s.lanes = c.lanes;
+    s.slice = c.slice;
+    s.slices = c.slices;
+    s.pixels = (int32_t)pixels;
+    s.channels = (int32_t)channels;
+    s.groups = (int32_t)groups;
+    s.d = (int32_t)(channels / groups);
+    s.parts = gn_parts(c.threads, c.slots, cells);
+    s.items = samples * blocks * c.slices;
+    s.per_xcd = (s.items + 7) / 8;
+    return s;
+}
+static unsigned gn_grid(const Slab& s) { return (unsigned)std::min<int64_t>(8 * s.per_xcd, GN_MOST_GRID); }
+
+template <typename F> static hipError_t with_lds(F* kernel, size_t bytes)
+{
+    return bytes <= 65536 ? hipSuccess : hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+}
+#define GN_TRY(e) do { const hipError_t _e = (e); if (_e != hipSuccess) return _e; } while (0)
+
+template <int CELLS> using Cells = std::integral_constant<int, CELLS>;
+// Rows of whole chunks whose halves lie in one group each; of whole chunks; any.
+template <typename F> static hipError_t by_columns(int64_t channels, int64_t groups, F&& launch)
+{
+    using Whole = std::false_type;
+    using Ragged = std::true_type;
+    if (channels % 8 != 0) return launch(Ragged(), Cells<8>());
+    return channels / groups % 4 == 0 ? launch(Whole(), Cells<2>()) : launch(Whole(), Cells<8>());
+}
+template <typename F> static hipError_t by_activation(int act, F&& launch)
+{
+    switch (act) {
+        case FF_ACT_RELU: return launch(std::integral_constant<int, FF_ACT_RELU>());
+        case FF_ACT_GELU: return launch(std::integral_constant<int, FF_ACT_GELU>());
+        case FF_ACT_SILU: return launch(std::integral_constant<int, FF_ACT_SILU>());
+        default: return launch(std::integral_constant<int, FF_ACT_IDENTITY>());
+    }
+}
+
+}  // namespace ffi

@@ -10,7 +10,9 @@
 namespace ffi {
 
 constexpr int GN_SPLIT_THREADS = 256;
-constexpr int GN_APPLY_ROWS = 4;      // pixels of a thread of the launches that apply what others have summed
+// Pixels of a thread: that holds its slab in registers, of the statistics' launch, and of the launches that apply what others have summed.
+constexpr int gn_rows(int size, bool backward) { return (size == 4 ? 4 : 8) / (backward ? 2 : 1); }
+constexpr int GN_STAT_ROWS = 8, GN_APPLY_ROWS = 4;
 constexpr int GN_MOST_GRID = 1 << 20; // workgroups of a launch; they take item after item
 constexpr size_t GN_MOST_LDS = 150 * 1024;
 
@@ -18,8 +20,8 @@ struct GnCut {
     int32_t threads, slots, lanes;   // of a workgroup
     int32_t slice, slices;           // columns of a slice, slices of a row
 };
-// Sums of a chunk that are kept apart: one where every chunk lies in one group, two where its halves do, else eight; of columns always eight.
-static int gn_cells(int64_t d, bool backward) { return backward ? 8 : d % 8 == 0 ? 1 : d % 4 == 0 ? 2 : 8; }
+// Sums of a chunk that are kept apart: two where its halves lie in one group each, else eight; of columns always eight.
+static int gn_cells(int64_t d, bool backward) { return !backward && d % 4 == 0 ? 2 : 8; }
 // threads that share the sum of a cell over the lanes, at most
 static int gn_parts(int threads, int64_t slots, int cells) { return (int)std::max<int64_t>(1, std::min<int64_t>(16, std::min<int64_t>(threads / slots, threads / (slots * cells)))); }
 // LDS of a workgroup: sums of two values per cell, of groups, and a row of weights
@@ -39,9 +41,6 @@ struct GnPlan {
 constexpr int64_t gn_gcd(int64_t a, int64_t b) { return b == 0 ? a : gn_gcd(b, a % b); }
 static int64_t gn_up(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
 
-// rows of a thread of the launch that holds its slab in registers
-static int gn_rows(int size, bool backward) { return size == 4 ? (backward ? 2 : 4) : (backward ? 4 : 8); }
-
 // size: bytes of an element; kept: a checkpoint is written or read, whose blocks of 32 columns lie in one workgroup; span: columns a row has to be covered to
 static GnPlan gn_plan(int64_t samples, int64_t pixels, int64_t channels, int64_t groups, int size, bool kept, int64_t span, bool backward)
 {
@@ -50,34 +49,36 @@ static GnPlan gn_plan(int64_t samples, int64_t pixels, int64_t channels, int64_t
     const int64_t row = gn_up(kept ? span : channels, unit);   // columns of a row with what is behind it
     const int rows = gn_rows(size, backward);
     // Slices from the narrowest on: as wide as 128 bytes, then wider while there are workgroups to spare and threads without a pixel, or none that fit.
-    for (int threads : {256, 1024}) {
-        int64_t best = 0;
+    // Of the numbers of threads the first that holds lines of 128 bytes, or else of 64, or any.
+    GnCut best = {};
+    for (int threads : {256, 512, 1024}) {
+        int64_t most = 0;
         for (int64_t w = std::min(step, row);; w = std::min(w + step, row)) {
             const int64_t slots = (w + 7) / 8;
             if (slots > threads || gn_lds(threads, slots, gn_cells(d, backward), d) > GN_MOST_LDS) break;
             const int64_t lanes = threads / slots, slices = (row + w - 1) / w;
             if ((pixels + lanes - 1) / lanes > rows) break;
-            best = w;
+            most = w;
             if (w >= row) break;
             const bool narrow = w * size < 128, idle = pixels * slots < 2 * threads && samples * slices > 1024;
             if (!narrow && !idle) break;
         }
-        if (best == 0) continue;
-        if (threads == 256 && best < row && best * size < 128) {   // wider lines in larger workgroups, where they hold them
-            const int64_t w = std::min(gn_up(128 / size, step), row), slots = (w + 7) / 8;
-            if (slots <= 1024 && gn_lds(1024, slots, gn_cells(d, backward), d) <= GN_MOST_LDS && (pixels + 1024 / slots - 1) / (1024 / slots) <= rows) continue;
-        }
-        const int32_t slots = (int32_t)((best + 7) / 8);
+        if (most == 0 || (best.slice > 0 && most <= best.slice)) continue;
+        const int32_t slots = (int32_t)((most + 7) / 8);
+        best = {threads, slots, threads / slots, (int32_t)most, (int32_t)((row + most - 1) / most)};
+        if (most * size >= 64 || most >= row) break;
+    }
+    if (best.slice > 0) {
         p.whole = true;
-        p.cut = {threads, slots, threads / slots, (int32_t)best, (int32_t)((row + best - 1) / best)};
+        p.cut = best;
         return p;
     }
-    // Statistics by slices of about 128 bytes, of whole groups or of an equal piece of one.
-    const int64_t wide = std::max<int64_t>(8, 128 / size);
+    // Statistics by slices of up to 256 columns, of whole groups or of an equal piece of one.
+    const int64_t wide = 256;
     int64_t w;
     p.pieces = 1;
     if (d <= wide) {
-        w = wide / d * d;
+        w = std::min(wide / d, groups) * d;
         p.stat.slices = (int32_t)((channels + w - 1) / w);
     } else {
         const int64_t pieces = (d + wide - 1) / wide;
@@ -89,7 +90,7 @@ static GnPlan gn_plan(int64_t samples, int64_t pixels, int64_t channels, int64_t
     p.stat.slice = (int32_t)w;
     p.stat.slots = (int32_t)((w + 7) / 8);
     p.stat.lanes = GN_SPLIT_THREADS / p.stat.slots;
-    const int64_t slots = std::min<int64_t>(gn_up(row, unit) / 8, std::max<int64_t>(unit / 8, 128 / size / 8));
+    const int64_t slots = std::min<int64_t>(row / 8, 32);
     p.cut.threads = GN_SPLIT_THREADS;
     p.cut.slots = (int32_t)slots;
     p.cut.lanes = (int32_t)(GN_SPLIT_THREADS / slots);
@@ -97,7 +98,7 @@ static GnPlan gn_plan(int64_t samples, int64_t pixels, int64_t channels, int64_t
     p.cut.slices = (int32_t)((row + p.cut.slice - 1) / p.cut.slice);
     p.apply_blocks = (int32_t)((pixels + (int64_t)p.cut.lanes * GN_APPLY_ROWS - 1) / ((int64_t)p.cut.lanes * GN_APPLY_ROWS));
     if (!backward) {
-        p.blocks = (int32_t)((pixels + (int64_t)p.stat.lanes * rows - 1) / ((int64_t)p.stat.lanes * rows));
+        p.blocks = (int32_t)((pixels + (int64_t)p.stat.lanes * GN_STAT_ROWS - 1) / ((int64_t)p.stat.lanes * GN_STAT_ROWS));
     } else {
         // sums of columns, whatever group they are of: the slices that apply, over as many blocks of pixels as keep every compute unit busy
         p.stat = p.cut;
