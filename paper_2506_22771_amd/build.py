@@ -23,10 +23,10 @@ OBJ_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libffint8.so")
 BIND = os.path.join(HERE, "_bind.so")
 SOURCES = ["elementwise.hip", "gemm_i8.hip", "gemm_few.hip", "conv.hip", "conv3.hip", "conv3_wide.hip", "wgrad3.hip", "rows.hip", "fused.hip", "api.hip",
-           "norm.hip", "ckpt.hip", "ckpt_wgrad.hip", "api_norm.hip", "gated.hip", "gated_grad.hip", "group_norm.hip", "group_norm_grad.hip", "dropout.hip", "api_blocks.hip"]
+           "norm.hip", "ckpt.hip", "ckpt_wgrad.hip", "api_norm.hip", "gated.hip", "gated_grad.hip", "group_norm.hip", "group_norm_f32.hip", "group_norm_bf16.hip", "group_norm_f16.hip", "dropout.hip", "api_blocks.hip"]
 HEADERS = [os.path.join(CSRC, "ff_internal.hpp"), os.path.join(CSRC, "device_math.hpp"), os.path.join(CSRC, "codes.hpp"), os.path.join(CSRC, "window.hpp"), os.path.join(CSRC, "ckpt.hpp"),
            os.path.join(CSRC, "act.hpp"), os.path.join(CSRC, "chunks.hpp"), os.path.join(CSRC, "norm.hpp"), os.path.join(CSRC, "norm_math.hpp"), os.path.join(CSRC, "api_checks.hpp"),
-           os.path.join(CSRC, "blocks.hpp"), os.path.join(CSRC, "group_norm.hpp"), os.path.join(CSRC, "group_norm_plan.hpp"), os.path.join(CSRC, "wgrad_plan.hpp"), os.path.join(os.path.dirname(HERE), "include", "ffint8.h")]
+           os.path.join(CSRC, "blocks.hpp"), os.path.join(CSRC, "group_norm.hpp"), os.path.join(CSRC, "group_norm_forward.hpp"), os.path.join(CSRC, "group_norm_backward.hpp"), os.path.join(CSRC, "group_norm_plan.hpp"), os.path.join(CSRC, "wgrad_plan.hpp"), os.path.join(os.path.dirname(HERE), "include", "ffint8.h")]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-ffp-contract=off", "-fno-fast-math",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-function", "-Wno-inline-asm"]
 

@@ -16,7 +16,7 @@ namespace ffi {
 template <typename T, int ACT, bool ANY = false> __device__ __forceinline__ void act_of(float u, float& f, float& d)
 {
     if constexpr (ACT == FF_ACT_RELU) {
-        f = u > 0 ? u : (u == u ? 0.0f : u);
+        f = u <= 0 ? 0.0f : u;   // (NaN stays)
         d = u > 0 ? 1.0f : (u == u ? 0.0f : u);
     } else if constexpr (ACT == FF_ACT_GELU) {
         const float e = __builtin_amdgcn_exp2f(u * u * -0.72134752044448170f);              // exp(-u^2 / 2)

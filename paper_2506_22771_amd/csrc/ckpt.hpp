@@ -249,11 +249,11 @@ __device__ __forceinline__ uint32_t ckpt_exponent(uint32_t amax_bits)
 }
 __device__ __forceinline__ float ckpt_scale(uint32_t e) { return __uint_as_float(e << 23); }   // e = 255: infinity, and 0 * it NaN
 
-// sr_head of elements at .. at + 7
-__device__ __forceinline__ void sr_words8(const SrKey& key, uint64_t at, uint32_t w[8])
+// sr_head of elements at .. at + 7; FOURS: at is a multiple of four
+template <bool FOURS = false> __device__ __forceinline__ void sr_words8(const SrKey& key, uint64_t at, uint32_t w[8])
 {
     const uint32_t lo = (uint32_t)at, k = key.k0 + (uint32_t)(at >> 32) * key.k1;
-    if ((lo & 3u) == 0) {
+    if (FOURS || (lo & 3u) == 0) {
         sr_head4(lo ^ k, w);
         sr_head4((lo + 4u) ^ (lo + 4u < lo ? k + key.k1 : k), w + 4);
     } else {
@@ -266,15 +266,15 @@ struct CkptRound {   // how codes are rounded; filled in by the launch
     SrKey key;
     int32_t stochastic;
 };
-// at: row-major element index of the chunk's first column
-__device__ __forceinline__ u32x2 ckpt_codes(const float v[8], uint32_t amax_bits, uint32_t e, const CkptRound& c, uint64_t at)
+// at: row-major element index of the chunk's first column (FOURS: a multiple of four)
+template <bool FOURS = false> __device__ __forceinline__ u32x2 ckpt_codes(const float v[8], uint32_t amax_bits, uint32_t e, const CkptRound& c, uint64_t at)
 {
     const uint32_t some = amax_bits >= (27u << 23) && amax_bits < 0x7F800000u ? 0xFFFFFFFFu : 0u;
     const float inv = __uint_as_float((254u - e) << 23);   // (not used where e is 127 or 255 for another reason)
     u32x2 q;
     if (c.stochastic) {
         uint32_t w[8];
-        sr_words8(c.key, at, w);
+        sr_words8<FOURS>(c.key, at, w);
         // what sr_scale makes of t = v * inv, of t 2^24 = v 2^p: one product less
         const int p = 151 - (int)e;
         uint32_t x[8];

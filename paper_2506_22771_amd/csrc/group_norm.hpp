@@ -26,23 +26,25 @@ struct Slab {
     int32_t slots, lanes, slice, slices;   // see GnCut
     int32_t pixels, channels, groups, d;
     int32_t parts;             // threads that share the sum of a cell over the lanes, at most
-    int64_t items, per_xcd;    // workgroups' work: (sample, [block of pixels,] slice)
+    int32_t first, items, per_xcd;   // workgroups' work, (sample, [block of pixels,] slice): this launch's.  (Fewer than there are chunks, which are fewer than 2^31.)
 };
-// Items in turn to the eight XCDs, so that neighbours, which share cache lines, meet in one L2; -1: none.
-__device__ __forceinline__ int64_t item_of(const Slab& s, int64_t turn)
+// A workgroup's item, or -1.  Items in turn to the eight XCDs, so that neighbours, which share cache lines, meet in one L2.
+__device__ __forceinline__ int item_of(const Slab& s)
 {
-    const int64_t i = (turn & 7) * s.per_xcd + (turn >> 3);
-    return i < s.items ? i : -1;
+    const int i = (int)(blockIdx.x & 7) * s.per_xcd + (int)(blockIdx.x >> 3);
+    return i < s.items ? s.first + i : -1;
 }
 
-// A thread's place in its slab.  Not to be traced back: the compiler would work out all that follows from it ahead of the loop over items, and keep it.
-__device__ __forceinline__ void place_of(const Slab& s, int& c, int& pl)
-{
-    uint32_t t = threadIdx.x;
-    opaque(t);
-    c = t % (uint32_t)s.slots;
-    pl = t / (uint32_t)s.slots;
-}
+// A thread's way through a matrix, from its chunk of its first pixel on.  (Step by step: products of the scalar step with every pixel's number are more scalars
+// than there are, and reading what was spilled of them took a tenth of all instructions.)
+template <typename P> struct Walk {
+    P *p, *first;
+    int64_t step;
+    __device__ __forceinline__ Walk(P* matrix, int64_t ld, int64_t pixel0, int lanes, bool there, int pl, int at)
+        : p(there ? element(matrix + pixel0 * ld, ld, 0, pl, at) : matrix + pixel0 * ld), first(p), step((int64_t)lanes * ld) {}
+    __device__ __forceinline__ void next() { p += step; }
+    __device__ __forceinline__ P* here(bool there) const { return there ? p : first; }   // a pixel that is not there: the first
+};
 
 // What the compiler is not to mix with what follows: several pixels' values at once take more registers than there are.
 __device__ __forceinline__ void one_pixel_at_a_time() { __builtin_amdgcn_sched_barrier(0); }
@@ -141,37 +143,6 @@ __device__ __forceinline__ float sum_block(float v, float* red)
     return s;
 }
 
-template <typename T> __device__ __forceinline__ void activate(int act, const float z[8], float f[8])
-{
-    float d;
-    switch (act) {   // (uniform)
-        case FF_ACT_RELU:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                act_of<T, FF_ACT_RELU, true>(z[i], f[i], d);
-                if (i & 1) one_pixel_at_a_time();
-            }
-            break;
-        case FF_ACT_GELU:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                act_of<T, FF_ACT_GELU, true>(z[i], f[i], d);
-                if (i & 1) one_pixel_at_a_time();
-            }
-            break;
-        case FF_ACT_SILU:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                act_of<T, FF_ACT_SILU, true>(z[i], f[i], d);
-                if (i & 1) one_pixel_at_a_time();
-            }
-            break;
-        default:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = z[i];
-    }
-}
-
 // ---- launches ----------------------------------------------------------------------------------------------------
 static Slab slab_of(const GnCut& c, int64_t samples, int64_t pixels, int64_t channels, int64_t groups, int64_t blocks, int cells)
 {
@@ -185,11 +156,22 @@ static Slab slab_of(const GnCut& c, int64_t samples, int64_t pixels, int64_t cha
     s.groups = (int32_t)groups;
     s.d = (int32_t)(channels / groups);
     s.parts = gn_parts(c.threads, c.slots, cells);
-    s.items = samples * blocks * c.slices;
-    s.per_xcd = (s.items + 7) / 8;
+    s.items = (int32_t)(samples * blocks * c.slices);
     return s;
 }
-static unsigned gn_grid(const Slab& s) { return (unsigned)std::min<int64_t>(8 * s.per_xcd, GN_MOST_GRID); }
+// A launch has fewer than 2^32 threads: one after the other for more items than that.
+template <typename Args, typename F> static hipError_t launch_items(Args a, F&& launch)
+{
+    const int64_t all = a.s.items;
+    for (int64_t first = 0; first < all; first += GN_MOST_GRID) {
+        a.s.first = (int32_t)first;
+        a.s.items = (int32_t)std::min<int64_t>(all - first, GN_MOST_GRID);
+        a.s.per_xcd = (a.s.items + 7) / 8;
+        launch((unsigned)(8 * a.s.per_xcd), a);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 
 template <typename F> static hipError_t with_lds(F* kernel, size_t bytes)
 {
@@ -215,5 +197,13 @@ template <typename F> static hipError_t by_activation(int act, F&& launch)
         default: return launch(std::integral_constant<int, FF_ACT_IDENTITY>());
     }
 }
+
+// group_norm.hip
+hipError_t launch_gn_join(const float4* part, float4* stats, const GroupNormForwardLaunch& f, int32_t parts, hipStream_t s);
+hipError_t launch_gn_goodness(const float* part, float* goodness, int64_t samples, int64_t parts, hipStream_t s);
+hipError_t launch_gn_params(const float2* sums, const GroupNormBackwardLaunch& g, hipStream_t s);
+// of one element type: group_norm_{f32,bf16,f16}.hip
+template <typename T> hipError_t gn_forward_typed(const GroupNormForwardLaunch& f, hipStream_t s);
+template <typename T> hipError_t gn_backward_typed(const GroupNormBackwardLaunch& g, hipStream_t s);
 
 }  // namespace ffi
