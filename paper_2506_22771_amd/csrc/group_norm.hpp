@@ -79,10 +79,9 @@ template <int CELLS, typename F> __device__ __forceinline__ void of_cells(int fi
 }
 
 // Sums over the lanes of K values of every cell, into lds[k * cells + i], cell i of the slots * CELLS.  lds: K cells (1 + parts + lanes) floats.  A barrier ends it.
-template <int K, int CELLS>
-__device__ __forceinline__ void sum_cells(const float (&v)[K][CELLS], int slots, int lanes, int most_parts, int c, int pl, float* lds)
+template <int K, int CELLS> __device__ __forceinline__ float* place_cells(const float (&v)[K][CELLS], int slots, int lanes, int most_parts, int c, int pl, float* lds)
 {
-    const int cells = slots * CELLS, parts = max(1, min(most_parts, (int)blockDim.x / (K * cells)));
+    const int cells = slots * CELLS;
     float* const all = lds + K * cells * (1 + most_parts);
     if (pl < lanes) {
 #pragma unroll
@@ -91,15 +90,23 @@ __device__ __forceinline__ void sum_cells(const float (&v)[K][CELLS], int slots,
             for (int i = 0; i < CELLS; ++i) all[(k * lanes + pl) * cells + c * CELLS + i] = v[k][i];
     }
     __syncthreads();
-    float* const some = lds + K * cells;
+    return all;
+}
+template <int K, int CELLS>
+__device__ __forceinline__ void sum_cells(const float (&v)[K][CELLS], int slots, int lanes, int most_parts, int c, int pl, float* lds)
+{
+    const int cells = slots * CELLS, parts = max(1, min(most_parts, (int)blockDim.x / (K * cells)));
+    const float* const all = place_cells(v, slots, lanes, most_parts, c, pl, lds);
+    float* const some = parts > 1 ? lds + K * cells : lds;
     for (int t = threadIdx.x; t < K * cells * parts; t += (int)blockDim.x) {
-        const int part = t / (K * cells), kc = t - part * (K * cells), k = kc >= cells && K > 1 ? kc / cells : 0, i = kc - k * cells;
+        const int part = t / (K * cells), kc = t - part * (K * cells), k = K > 1 && kc >= cells ? 1 : 0, i = kc - k * cells;
         float s = 0;
 #pragma unroll 4
         for (int l = part; l < lanes; l += parts) s += all[(k * lanes + l) * cells + i];
         some[t] = s;
     }
     __syncthreads();
+    if (parts == 1) return;
     for (int t = threadIdx.x; t < K * cells; t += (int)blockDim.x) {
         float s = 0;
 #pragma unroll 4
@@ -113,14 +120,14 @@ template <int K, typename F> __device__ __forceinline__ void sum_groups(int grou
 {
     if (n <= 16) {
         for (int t = threadIdx.x; t < K * groups; t += (int)blockDim.x) {
-            const int k = K > 1 ? t / groups : 0, g = t - k * groups;
+            const int k = K > 1 && t >= groups ? 1 : 0, g = t - k * groups;
             float s = 0;
             for (int i = 0; i < n; ++i) s += value(k, g * n + i);
             out[t] = s;
         }
     } else {
         for (int t = threadIdx.x >> 6; t < K * groups; t += (int)blockDim.x / 64) {
-            const int k = K > 1 ? t / groups : 0, g = t - k * groups;
+            const int k = K > 1 && t >= groups ? 1 : 0, g = t - k * groups;
             float s = 0;
             for (int i = threadIdx.x & 63; i < n; i += 64) s += value(k, g * n + i);
             s = wave_sum(s);
@@ -128,6 +135,26 @@ template <int K, typename F> __device__ __forceinline__ void sum_groups(int grou
         }
     }
     __syncthreads();
+}
+// Both at once, for sums of cells that nobody else asks for: out[k * groups + g], K up to 2.  A barrier ends it.
+template <int K, int CELLS>
+__device__ __forceinline__ void sum_lanes_of_groups(const float (&v)[K][CELLS], int slots, int lanes, int most_parts, int c, int pl, int groups, int n, float* lds, float* out)
+{
+    const int cells = slots * CELLS;
+    if (lanes * n <= 16) {   // few values to a group: one step, a thread each
+        const float* const all = place_cells(v, slots, lanes, most_parts, c, pl, lds);
+        for (int t = threadIdx.x; t < K * groups; t += (int)blockDim.x) {
+            const int k = K > 1 && t >= groups ? 1 : 0, g = t - k * groups;
+            float s = 0;
+            for (int l = 0; l < lanes; ++l)
+                for (int i = 0; i < n; ++i) s += all[(k * lanes + l) * cells + g * n + i];
+            out[t] = s;
+        }
+        __syncthreads();
+    } else {
+        sum_cells<K, CELLS>(v, slots, lanes, most_parts, c, pl, lds);
+        sum_groups<K>(groups, n, out, [&](int k, int i) { return lds[k * cells + i]; });
+    }
 }
 
 // Sum of a workgroup's values, in thread 0.  red: a word per wavefront.  A barrier begins it.

@@ -118,10 +118,9 @@ __device__ __forceinline__ void store_dx(T* to, int n, const float h[8], const f
     store8(to, RAGGED ? n : 8, v);
 }
 
-template <typename T, bool RAGGED, bool FROM_X, int CELLS, int ACT>
-__global__ __launch_bounds__(1024, 4) void k_gn_backward(GnBackwardArgs<T> a)
+// U: pixels of a thread
+template <typename T, bool RAGGED, bool FROM_X, int CELLS, int ACT, int U> __global__ __launch_bounds__(1024, 4) void k_gn_backward(GnBackwardArgs<T> a)
 {
-    constexpr int U = gn_rows(sizeof(T), true);
     extern __shared__ __attribute__((aligned(16))) float lds[];
     const Slab& s = a.s;
     const int item = item_of(s);
@@ -133,24 +132,20 @@ __global__ __launch_bounds__(1024, 4) void k_gn_backward(GnBackwardArgs<T> a)
     const int64_t pixel0 = (int64_t)sample * s.pixels;
     GnFrom<T, FROM_X> from(a, pixel0, pl, chunk, n > 0 && pl < s.pixels);
     GnPixel<T, FROM_X> px[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        from.template load<RAGGED>(a, px[u], pl + u * s.lanes < s.pixels ? n : 0);
-    }
     GnGradChunk<T, FROM_X, CELLS> p;
+    float v[2][8] = {};
+#pragma unroll
+    for (int u = 0; u < U; ++u) from.template load<RAGGED>(a, px[u], pl + u * s.lanes < s.pixels ? n : 0);
     load_chunk(a, p, sample, chunk, n, 8 * c, c0 / s.d, groups);
-    // where f' takes more than a comparison dz is kept between the two times that it is needed
-    constexpr bool KEEP = ACT == FF_ACT_GELU || ACT == FF_ACT_SILU;
-    float v[2][8] = {}, dz[KEEP ? U : 1][8];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if (n > 0 && pl + u * s.lanes < s.pixels) {
-            float h[8];
+            float h[8], dz[8];
             h_of(px[u], p, h);
-            dz_of<ACT>(px[u], p, h, dz[KEEP ? u : 0]);
-            add_column_sums<RAGGED>(h, dz[KEEP ? u : 0], n, v);
+            dz_of<ACT>(px[u], p, h, dz);
+            add_column_sums<RAGGED>(h, dz, n, v);
         }
-        if constexpr (!KEEP) opaque(px[u].dy);
+        opaque(px[u].dy);
         if constexpr (FROM_X) opaque(px[u].x);
         else opaque(px[u].q);
         one_pixel_at_a_time();
@@ -175,10 +170,10 @@ __global__ __launch_bounds__(1024, 4) void k_gn_backward(GnBackwardArgs<T> a)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (n > 0 && pl + u * s.lanes < s.pixels) {
-                float h[8];
+                float h[8], dz[8];
                 h_of(px[u], p, h);
-                if constexpr (!KEEP) dz_of<ACT>(px[u], p, h, dz[0]);
-                store_dx<T, RAGGED, FROM_X, CELLS>(to.p, n, h, dz[KEEP ? u : 0], p, sg, sh);
+                dz_of<ACT>(px[u], p, h, dz);
+                store_dx<T, RAGGED, FROM_X, CELLS>(to.p, n, h, dz, p, sg, sh);
             }
             to.next();
             one_pixel_at_a_time();
@@ -315,7 +310,8 @@ template <typename T, bool RAGGED, bool FROM_X, int CELLS, int ACT> static hipEr
         a.sums = g.dweight || g.dbias ? sums : nullptr;
         a.s = slab_of(p.cut, g.samples, g.pixels, g.channels, g.groups, 1, 8);
         const size_t lds = gn_lds(p.cut.threads, p.cut.slots, 8, d);
-        auto* const kernel = k_gn_backward<T, RAGGED, FROM_X, CELLS, ACT>;
+        constexpr int U = gn_rows(sizeof(T), true), FEW = RAGGED ? U : U / 4;
+        auto* const kernel = p.cut.lanes * FEW >= g.pixels ? k_gn_backward<T, RAGGED, FROM_X, CELLS, ACT, FEW> : k_gn_backward<T, RAGGED, FROM_X, CELLS, ACT, U>;
         GN_TRY(with_lds(kernel, lds));
         GN_TRY(launch_items(a, [&](unsigned grid, const auto& part) { kernel<<<grid, p.cut.threads, lds, s>>>(part); }));
     } else {

@@ -22,6 +22,7 @@ template <typename T> struct GnForwardArgs {
     const float4* stats;   // launch that applies: mean, its rest, rstd
     CkptPtr k;
     SrKey key;
+    int32_t pad_steps;     // bytes of a row's exponents' pad that a chunk's lane writes, at most
     int32_t param_f32, pieces, blocks, rows;   // rows: pixels of a workgroup
     float eps, inv_m;
 };
@@ -88,8 +89,10 @@ __device__ __forceinline__ float finish_chunk(const GnForwardArgs<T>& a, const G
         uint8_t* const row = to.e.p;
         const int block = chunk >> 2;
         if ((chunk & 3) == 0 && block < a.k.blocks) row[block] = (uint8_t)e;
-#pragma nounroll
-        for (int pad = a.k.blocks + chunk; pad < (int)a.k.epitch; pad += slots) row[pad] = 0;
+        int pad = a.k.blocks + chunk;
+#pragma clang loop unroll(disable) vectorize(disable) interleave(disable)
+        for (int i = 0; i < a.pad_steps; ++i, pad += slots)
+            if (pad < (int)a.k.epitch) row[pad] = 0;
     }
     if (n <= 0) return 0.0f;
 #pragma unroll
@@ -108,9 +111,9 @@ __device__ __forceinline__ float finish_chunk(const GnForwardArgs<T>& a, const G
     return s;
 }
 
-template <typename T, bool RAGGED, GnKept KEPT, int CELLS, int ACT> __global__ __launch_bounds__(1024, 4) void k_gn_forward(GnForwardArgs<T> a)
+// U: pixels of a thread
+template <typename T, bool RAGGED, GnKept KEPT, int CELLS, int ACT, int U> __global__ __launch_bounds__(1024, 4) void k_gn_forward(GnForwardArgs<T> a)
 {
-    constexpr int U = gn_rows(sizeof(T), false);
     extern __shared__ __attribute__((aligned(16))) float lds[];
     const Slab& s = a.s;
     const int row_slots = KEPT != KEPT_NONE ? (int)((a.k.pitch + 31) / 32 * 4) : (s.channels + 7) / 8;
@@ -125,13 +128,13 @@ template <typename T, bool RAGGED, GnKept KEPT, int CELLS, int ACT> __global__ _
     // a chunk that does not exist is read from a place that does, and not used
     Walk<const T> x(a.x, a.ldx, pixel0, s.lanes, n > 0 && pl < s.pixels, pl, 8 * chunk);
     Raw8<T> raw[U];
+    float v[1][CELLS] = {}, v2[2][CELLS] = {}, m[CELLS];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const bool there = n > 0 && pl + u * s.lanes < s.pixels;
         raw[u] = load_raw(x.here(there), RAGGED ? (there ? n : 0) : 8);
         x.next();
     }
-    float v[1][CELLS] = {}, v2[2][CELLS] = {}, m[CELLS];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if (n > 0 && pl + u * s.lanes < s.pixels) {
@@ -145,8 +148,7 @@ template <typename T, bool RAGGED, GnKept KEPT, int CELLS, int ACT> __global__ _
     }
     const int per_group = s.d * CELLS / 8;
     float* const out = lds + 2 * s.slots * CELLS * (1 + s.parts + s.lanes);
-    sum_cells<1, CELLS>(v, s.slots, s.lanes, s.parts, c, pl, lds);
-    sum_groups<1>(groups, per_group, out, [&](int, int i) { return lds[i]; });
+    sum_lanes_of_groups(v, s.slots, s.lanes, s.parts, c, pl, groups, per_group, lds, out);
     of_cells<CELLS>(8 * c, s.d, groups, [&](int i, int g, int) { m[i] = out[g] * a.inv_m; });
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -163,12 +165,10 @@ template <typename T, bool RAGGED, GnKept KEPT, int CELLS, int ACT> __global__ _
         opaque(raw[u]);
         one_pixel_at_a_time();
     }
-    const int cells = s.slots * CELLS;
-    sum_cells<2, CELLS>(v2, s.slots, s.lanes, s.parts, c, pl, lds);
     GnChunk<T, CELLS> p;
     load_param<T>(a.weight, a.param_f32, 8 * (int64_t)chunk, n, 1.0f, p.w);
     load_param<T>(a.bias, a.param_f32, 8 * (int64_t)chunk, n, 0.0f, p.b);
-    sum_groups<2>(groups, per_group, out, [&](int k, int i) { return lds[k * cells + i]; });
+    sum_lanes_of_groups(v2, s.slots, s.lanes, s.parts, c, pl, groups, per_group, lds, out);
     of_cells<CELLS>(8 * c, s.d, groups, [&](int i, int g, int at) {
         const float square = out[groups + g] * a.inv_m, rest = mean_rest(m[i], out[g] * a.inv_m, square);
         p.mean(i, m[i], rest);
@@ -234,8 +234,7 @@ template <typename T, bool RAGGED, int CELLS> __global__ __launch_bounds__(GN_SP
     const int cells = s.slots * CELLS, per_group = one ? cells : s.d * CELLS / 8, d = one ? 8 * s.slots : s.d;
     const float count = (float)(pixels * (one ? cols : s.d)), inv = 1.0f / count;
     float* const out = lds + 2 * cells * (1 + s.parts + s.lanes);
-    sum_cells<1, CELLS>(v, s.slots, s.lanes, s.parts, c, pl, lds);
-    sum_groups<1>(groups, per_group, out, [&](int, int i) { return lds[i]; });
+    sum_lanes_of_groups(v, s.slots, s.lanes, s.parts, c, pl, groups, per_group, lds, out);
     of_cells<CELLS>(8 * c, d, groups, [&](int i, int g, int) { m[i] = out[g] * inv; });
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -250,8 +249,7 @@ template <typename T, bool RAGGED, int CELLS> __global__ __launch_bounds__(GN_SP
             }
         }
     }
-    sum_cells<2, CELLS>(v2, s.slots, s.lanes, s.parts, c, pl, lds);
-    sum_groups<2>(groups, per_group, out, [&](int k, int i) { return lds[k * cells + i]; });
+    sum_lanes_of_groups(v2, s.slots, s.lanes, s.parts, c, pl, groups, per_group, lds, out);
     of_cells<CELLS>(8 * c, d, groups, [&](int i, int g, int at) {
         if (pl == 0 && at == 0 && i * (8 / CELLS) < n) {
             const float rest = out[g] * inv;
@@ -324,6 +322,8 @@ template <typename T, bool RAGGED, GnKept KEPT, int CELLS, int ACT> static hipEr
     if (KEPT != KEPT_NONE) {
         a.k = ckpt_ptr(f.q, f.e, f.channels);
         a.key = make_sr_key(f.seed, f.tag);
+        const int64_t row_slots = (a.k.pitch + 31) / 32 * 4;
+        a.pad_steps = (int32_t)((a.k.epitch - a.k.blocks + row_slots - 1) / row_slots);
     }
     float* good;
     int64_t parts;
@@ -333,7 +333,8 @@ template <typename T, bool RAGGED, GnKept KEPT, int CELLS, int ACT> static hipEr
         a.good = f.goodness ? good : nullptr;
         a.s = slab_of(p.cut, f.samples, f.pixels, f.channels, f.groups, 1, CELLS);
         const size_t lds = gn_lds(p.cut.threads, p.cut.slots, CELLS, d);
-        auto* const kernel = k_gn_forward<T, RAGGED, KEPT, CELLS, ACT>;
+        constexpr int U = gn_rows(sizeof(T), false), FEW = RAGGED ? U : U / 4;
+        auto* const kernel = p.cut.lanes * FEW >= f.pixels ? k_gn_forward<T, RAGGED, KEPT, CELLS, ACT, FEW> : k_gn_forward<T, RAGGED, KEPT, CELLS, ACT, U>;
         GN_TRY(with_lds(kernel, lds));
         GN_TRY(launch_items(a, [&](unsigned grid, const auto& part) { kernel<<<grid, p.cut.threads, lds, s>>>(part); }));
     } else {

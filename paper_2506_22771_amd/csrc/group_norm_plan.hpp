@@ -11,7 +11,7 @@ namespace ffi {
 
 constexpr int GN_SPLIT_THREADS = 256;
 // Pixels of a thread: that holds its slab in registers, of the statistics' launch, and of the launches that apply what others have summed.
-constexpr int gn_rows(int size, bool backward) { return (size == 4 ? 4 : 8) / (backward ? 2 : 1); }
+constexpr int gn_rows(int size, bool backward) { return backward ? (size == 4 ? 4 : 8) : (size == 4 ? 8 : 16); }
 constexpr int GN_STAT_ROWS = 8, GN_APPLY_ROWS = 4;
 constexpr int GN_MOST_GRID = 1 << 20; // workgroups of a launch; they take item after item
 constexpr size_t GN_MOST_LDS = 150 * 1024;
@@ -50,6 +50,7 @@ static GnPlan gn_plan(int64_t samples, int64_t pixels, int64_t channels, int64_t
     const int rows = gn_rows(size, backward);
     // Slices from the narrowest on: as wide as 128 bytes, then wider while there are workgroups to spare and threads without a pixel, or none that fit.
     // Of the numbers of threads the first that holds lines of 128 bytes, or else of 64, or any.
+    const int64_t enough = kept ? 128 : 64;
     GnCut best = {};
     for (int threads : {256, 512, 1024}) {
         int64_t most = 0;
@@ -66,7 +67,7 @@ static GnPlan gn_plan(int64_t samples, int64_t pixels, int64_t channels, int64_t
         if (most == 0 || (best.slice > 0 && most <= best.slice)) continue;
         const int32_t slots = (int32_t)((most + 7) / 8);
         best = {threads, slots, threads / slots, (int32_t)most, (int32_t)((row + most - 1) / most)};
-        if (most * size >= 64 || most >= row) break;
+        if (most * size >= enough || most >= row) break;
     }
     if (best.slice > 0) {
         p.whole = true;
