@@ -218,33 +218,63 @@ template <typename T, bool RAGGED, bool FROM_X, int CELLS, int ACT> __global__ _
     for (int t = threadIdx.x; t < cols; t += (int)blockDim.x) a.sums[(int64_t)sb * s.channels + c0 + t] = make_float2(lds[t], lds[8 * s.slots + t]);
 }
 
-// Sums of a sample's blocks, a wavefront for a group: sums of its columns, and those of the group by its size.
+// Sums of a sample's blocks: sums of its columns, and those of its groups by a group's size.  A workgroup takes `many` groups of up to 64 columns together, or one
+// in tiles of 64 columns, sixteen threads to a column.
 template <typename T>
-__global__ __launch_bounds__(256) void k_gn_backward_join(const float2* part, float2* sums, float2* group, const void* weight, int param_f32, int64_t samples,
-                                                          int32_t groups, int32_t d, int32_t blocks, float inv_m)
+__global__ __launch_bounds__(1024) void k_gn_backward_join(const float2* part, float2* sums, float2* group, const void* weight, int param_f32, int64_t items,
+                                                           int32_t per_sample, int32_t groups, int32_t d, int32_t many, int32_t blocks, float inv_m)
 {
-    const int lane = threadIdx.x & 63, channels = groups * d;
-    for (int64_t sg = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); sg < samples * groups; sg += (int64_t)gridDim.x * 4) {
-        const int64_t sample = sg / groups;
-        const int c0 = (int)(sg - sample * groups) * d;
+    __shared__ float2 red[16][64];
+    const int col = threadIdx.x & 63, lane = threadIdx.x >> 6, channels = groups * d;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t sample = item / per_sample;
+        const int g0 = (int)(item - sample * per_sample) * many, here = min(many, groups - g0), c0 = g0 * d, cols = here * d;
         float2 of_group = make_float2(0, 0);
-        for (int i = lane; i < d; i += 64) {
+        for (int first = 0; first < cols; first += 64) {
+            const int c = first + col;
             float2 t = make_float2(0, 0);
-#pragma unroll 8
-            for (int b = 0; b < blocks; ++b) {
-                const float2 v = part[(sample * blocks + b) * channels + c0 + i];
-                t.x += v.x;
-                t.y += v.y;
+            if (c < cols)
+#pragma unroll 4
+                for (int b = lane; b < blocks; b += 16) {
+                    const float2 v = part[(sample * blocks + b) * channels + c0 + c];
+                    t.x += v.x;
+                    t.y += v.y;
+                }
+            __syncthreads();   // (what the last tile left in red has been read)
+            red[lane][col] = t;
+            __syncthreads();
+            if (lane == 0) {
+                for (int l = 1; l < 16; ++l) {
+                    t.x += red[l][col].x;
+                    t.y += red[l][col].y;
+                }
+                float w[8] = {};
+                if (c < cols) {
+                    sums[sample * channels + c0 + c] = t;
+                    load_param<T>(weight, param_f32, c0 + c, 1, 1.0f, w);
+                }
+                t = make_float2(w[0] * t.x, w[0] * t.y);   // (zero behind the last column)
+                if (here > 1) {
+                    red[0][col] = t;
+                } else {
+                    of_group.x += wave_sum(t.x);
+                    of_group.y += wave_sum(t.y);
+                }
             }
-            float w[8];
-            load_param<T>(weight, param_f32, c0 + i, 1, 1.0f, w);
-            sums[sample * channels + c0 + i] = t;
-            of_group.x = __builtin_fmaf(w[0], t.x, of_group.x);
-            of_group.y = __builtin_fmaf(w[0], t.y, of_group.y);
         }
-        of_group.x = wave_sum(of_group.x);
-        of_group.y = wave_sum(of_group.y);
-        if (lane == 0) group[sg] = make_float2(of_group.x * inv_m, of_group.y * inv_m);
+        if (here > 1) {
+            __syncthreads();
+            for (int g = threadIdx.x; g < here; g += 1024) {
+                for (int i = 0; i < d; ++i) {
+                    of_group.x += red[0][g * d + i].x;
+                    of_group.y += red[0][g * d + i].y;
+                }
+                group[sample * groups + g0 + g] = make_float2(of_group.x * inv_m, of_group.y * inv_m);
+                of_group = make_float2(0, 0);
+            }
+        } else if (threadIdx.x == 0) {
+            group[sample * groups + g0] = make_float2(of_group.x * inv_m, of_group.y * inv_m);
+        }
     }
 }
 
@@ -323,9 +353,9 @@ template <typename T, bool RAGGED, bool FROM_X, int CELLS, int ACT> static hipEr
         a.s = slab_of(p.stat, g.samples, g.pixels, g.channels, g.groups, p.blocks, 8);
         const size_t lds = gn_lds(p.stat.threads, p.stat.slots, 8, d);
         GN_TRY(launch_items(a, [&](unsigned grid, const auto& part) { k_gn_backward_sums<T, RAGGED, FROM_X, CELLS, ACT><<<grid, GN_SPLIT_THREADS, lds, s>>>(part); }));
-        const int64_t all = g.samples * g.groups;
-        k_gn_backward_join<T><<<(unsigned)std::min<int64_t>((all + 3) / 4, GN_MOST_GRID), 256, 0, s>>>(part, sums, group, g.weight, a.param_f32, g.samples,
-                                                                                                (int32_t)g.groups, (int32_t)d, p.blocks, a.inv_m);
+        const int64_t many = std::max<int64_t>(1, std::min(g.groups, 64 / d)), per_sample = (g.groups + many - 1) / many, items = g.samples * per_sample;
+        k_gn_backward_join<T><<<(unsigned)std::min<int64_t>(items, GN_MOST_GRID), 1024, 0, s>>>(part, sums, group, g.weight, a.param_f32, items, (int32_t)per_sample,
+                                                                                       (int32_t)g.groups, (int32_t)d, (int32_t)many, p.blocks, a.inv_m);
         GN_TRY(hipGetLastError());
         if (g.dx) {
             a.group = group;

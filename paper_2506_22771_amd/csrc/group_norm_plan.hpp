@@ -23,7 +23,7 @@ struct GnCut {
 // Sums of a chunk that are kept apart: two where its halves lie in one group each, else eight; of columns always eight.
 static int gn_cells(int64_t d, bool backward) { return !backward && d % 4 == 0 ? 2 : 8; }
 // threads that share the sum of a cell over the lanes, at most
-static int gn_parts(int threads, int64_t slots, int cells) { return (int)std::max<int64_t>(1, std::min<int64_t>(16, std::min<int64_t>(threads / slots, threads / (slots * cells)))); }
+static int gn_parts(int threads, int64_t slots, int cells) { return (int)std::max<int64_t>(1, std::min<int64_t>(32, std::min<int64_t>(threads / slots, threads / (slots * cells)))); }
 // LDS of a workgroup: sums of two values per cell, of groups, and a row of weights
 static size_t gn_lds(int threads, int64_t slots, int cells, int64_t d)
 {
@@ -68,6 +68,20 @@ static GnPlan gn_plan(int64_t samples, int64_t pixels, int64_t channels, int64_t
         const int32_t slots = (int32_t)((most + 7) / 8);
         best = {threads, slots, threads / slots, (int32_t)most, (int32_t)((row + most - 1) / most)};
         if (most * size >= enough || most >= row) break;
+    }
+    // Fewer workgroups than compute units: narrower slices, and all the threads there are, for the shortest way through.
+    const int64_t units = 256;
+    if (best.slice > 0 && samples * best.slices < units) {
+        int64_t w = std::min(step, row);
+        while (w < row && samples * ((row + w - 1) / w) > units) w = std::min(w + step, row);
+        const int64_t slots = (w + 7) / 8;
+        for (int threads : {1024, 512, 256}) {
+            if (w > best.slice || slots > threads || gn_lds(threads, slots, gn_cells(d, backward), d) > GN_MOST_LDS) continue;
+            if (threads > 256 && threads / 2 >= pixels * slots) continue;   // (half of them would do)
+            if ((pixels + threads / slots - 1) / (threads / slots) > rows) continue;
+            best = {threads, (int32_t)slots, (int32_t)(threads / slots), (int32_t)w, (int32_t)((row + w - 1) / w)};
+            break;
+        }
     }
     if (best.slice > 0) {
         p.whole = true;
