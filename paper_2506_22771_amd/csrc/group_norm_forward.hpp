@@ -333,7 +333,7 @@ template <typename T, bool RAGGED, GnKept KEPT, int CELLS, int ACT> static hipEr
         a.good = f.goodness ? good : nullptr;
         a.s = slab_of(p.cut, f.samples, f.pixels, f.channels, f.groups, 1, CELLS);
         const size_t lds = gn_lds(p.cut.threads, p.cut.slots, CELLS, d);
-        constexpr int U = gn_rows(sizeof(T), false), FEW = RAGGED ? U : U / 4;
+        constexpr int U = gn_rows(sizeof(T), false), FEW = U / 4;
         auto* const kernel = p.cut.lanes * FEW >= f.pixels ? k_gn_forward<T, RAGGED, KEPT, CELLS, ACT, FEW> : k_gn_forward<T, RAGGED, KEPT, CELLS, ACT, U>;
         GN_TRY(with_lds(kernel, lds));
         GN_TRY(launch_items(a, [&](unsigned grid, const auto& part) { kernel<<<grid, p.cut.threads, lds, s>>>(part); }));

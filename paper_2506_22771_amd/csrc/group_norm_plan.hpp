@@ -10,7 +10,8 @@
 namespace ffi {
 
 constexpr int GN_SPLIT_THREADS = 256;
-// Pixels of a thread: that holds its slab in registers, of the statistics' launch, and of the launches that apply what others have summed.
+// Pixels of a thread: that holds its slab in registers, of the statistics' launch, and of the launches that apply what others have summed.  As many as 128 registers hold
+// beside the sums.  512 x 32x32 x 128 bf16 forward 62 us with 16 and 70 with 8, backward from codes 112 with 8 and 124 with 16 and 168 registers, three wavefronts a SIMD.
 constexpr int gn_rows(int size, bool backward) { return backward ? (size == 4 ? 4 : 8) : (size == 4 ? 8 : 16); }
 constexpr int GN_STAT_ROWS = 8, GN_APPLY_ROWS = 4;
 constexpr int GN_MOST_GRID = 1 << 20; // workgroups of a launch; they take item after item
@@ -49,7 +50,8 @@ static GnPlan gn_plan(int64_t samples, int64_t pixels, int64_t channels, int64_t
     const int64_t row = gn_up(kept ? span : channels, unit);   // columns of a row with what is behind it
     const int rows = gn_rows(size, backward);
     // Slices from the narrowest on: as wide as 128 bytes, then wider while there are workgroups to spare and threads without a pixel, or none that fit.
-    // Of the numbers of threads the first that holds lines of 128 bytes, or else of 64, or any.
+    // Of the numbers of threads the first that holds lines of 128 bytes (of 64 where no codes are written), or else the widest of any: workgroups that are small run beside others,
+    // whose loads, sums and stores overlap, but rows in pieces of 32 bytes are slow (512 x 32x32 x 128 bf16 forward 62 us in pieces of 64 bytes, 76 in those of 32).
     const int64_t enough = kept ? 128 : 64;
     GnCut best = {};
     for (int threads : {256, 512, 1024}) {
@@ -69,7 +71,7 @@ static GnPlan gn_plan(int64_t samples, int64_t pixels, int64_t channels, int64_t
         best = {threads, slots, threads / slots, (int32_t)most, (int32_t)((row + most - 1) / most)};
         if (most * size >= enough || most >= row) break;
     }
-    // Fewer workgroups than compute units: narrower slices, and all the threads there are, for the shortest way through.
+    // Fewer workgroups than compute units: narrower slices, and all the threads there are, for the shortest way through (1 x 32x32 x 128 bf16 9.8 us, by the rule above 13.1).
     const int64_t units = 256;
     if (best.slice > 0 && samples * best.slices < units) {
         int64_t w = std::min(step, row);

@@ -216,7 +216,7 @@ def two_sets(batch: int, image: Tuple[int, int, int], seed: int, device="cuda", 
     return sets
 
 
-def main(steps: int = 60, image: Tuple[int, int, int] = (32, 32, 3), batch: int = 64, lam: float = 0.05, lr: float = 0.03, report: Optional[int] = 10) -> List[float]:
+def main(steps: int = 200, image: Tuple[int, int, int] = (32, 32, 3), batch: int = 64, lam: float = 0.05, lr: float = 3e-4, report: Optional[int] = 25) -> List[float]:
     net = GatedNet(image, ((4, 64, 8), (2, 128, 16)), (256, 256), batch)
     history = []
     for t in range(steps):

@@ -29,7 +29,7 @@ def inputs(samples, pixels, channels, dtype, seed=0):
     return typed(x, dtype), typed(dy, dtype), 1 + 0.3 * rng.standard_normal(channels), 0.3 * rng.standard_normal(channels), coeff
 
 
-# Sums: a thread adds up to eight pixels and eight columns, a sum over the lanes has up to 64 terms and 16 parts, one over a group's columns up to 64 a lane
+# Sums: a thread adds up to 64 values (sixteen pixels of four columns), a sum over the lanes has up to 64 terms and their parts' sums, one over a group's columns up to 64 a lane
 # and six levels (groups of up to 4096 columns beside each other; longer ones are joined in 64 bits): D roundings of the sum of magnitudes at most.
 D = 170
 
