@@ -227,8 +227,8 @@ template <typename T> __global__ __launch_bounds__(WAVES * 64) void k_gated_few(
 // wavefronts issue a step's copies before its last multiplies and half after them.  A wavefront has the same 32 columns of both projections, which is one
 // checkpoint block: its exponent takes a maximum inside a lane and one exchange.  A workgroup takes tile after tile, the next one's first copies under way
 // during the epilogue; tiles go to an XCD in blocks of eight rows of tiles, which share operands in its L2.
-// 16384 x 4096 x 4096 bf16, kept: 520 to 560 us, 1.10e12 operations at 2.0 to 2.1 POP/s, where a library's int8 product alone takes 558; the matrix pipe is busy for 52 % of the
-// clocks it gets, and reads of LDS, at 12 fragments to 16 multiplies, for most of the rest.
+// 16384 x 4096 x 4096 bf16, kept: 520 to 560 us, 1.10e12 operations at 2.0 to 2.1 POP/s, where a library's int8 product alone takes 558.  The matrix pipe is busy for 53 % of the clocks
+// (beside it, LDS reads take 384 of every 512: six fragments to eight multiplies), and 280 MB of stores are 50 us.
 // ------------------------------------------------------------------------------------------------
 template <int N> __device__ __forceinline__ void wait_copies()   // all but N of this wavefront's copies and stores
 {

@@ -328,8 +328,8 @@ template <typename T, bool RAGGED, GnKept KEPT, int CELLS, int ACT> static hipEr
     float* good;
     int64_t parts;
     if (p.whole) {
-        good = (float*)f.ws;
         parts = p.cut.slices;
+        good = parts == 1 ? f.goodness : (float*)f.ws;   // (one part is the sum)
         a.good = f.goodness ? good : nullptr;
         a.s = slab_of(p.cut, f.samples, f.pixels, f.channels, f.groups, 1, CELLS);
         const size_t lds = gn_lds(p.cut.threads, p.cut.slots, CELLS, d);
@@ -340,8 +340,8 @@ template <typename T, bool RAGGED, GnKept KEPT, int CELLS, int ACT> static hipEr
     } else {
         float4* const part = (float4*)f.ws;
         float4* const stats = part + f.samples * f.groups * p.pieces * p.blocks;
-        good = (float*)(stats + f.samples * f.groups);
         parts = (int64_t)p.cut.slices * p.apply_blocks;
+        good = parts == 1 ? f.goodness : (float*)(stats + f.samples * f.groups);
         a.part = part;
         a.stats = stats;
         a.pieces = p.pieces;
@@ -363,7 +363,7 @@ template <typename T, bool RAGGED, GnKept KEPT, int CELLS, int ACT> static hipEr
         a.s = slab_of(p.cut, f.samples, f.pixels, f.channels, f.groups, p.apply_blocks, CELLS);
         GN_TRY(launch_items(a, [&](unsigned grid, const auto& part) { k_gn_apply<T, RAGGED, KEPT, CELLS, ACT><<<grid, GN_SPLIT_THREADS, 0, s>>>(part); }));
     }
-    return f.goodness ? launch_gn_goodness(good, f.goodness, f.samples, parts, s) : hipSuccess;
+    return f.goodness && parts > 1 ? launch_gn_goodness(good, f.goodness, f.samples, parts, s) : hipSuccess;
 }
 template <typename T> hipError_t gn_forward_typed(const GroupNormForwardLaunch& f, hipStream_t s)
 {

@@ -11,7 +11,7 @@ namespace ffi {
 
 constexpr int GN_SPLIT_THREADS = 256;
 // Pixels of a thread: that holds its slab in registers, of the statistics' launch, and of the launches that apply what others have summed.  As many as 128 registers hold
-// beside the sums.  512 x 32x32 x 128 bf16 forward 62 us with 16 and 70 with 8, backward from codes 112 with 8 and 124 with 16 and 168 registers, three wavefronts a SIMD.
+// beside the sums.  512 x 32x32 x 128 bf16 forward 62 us with 16 and 72 with 8, backward from codes 111 with 8 and 124 with 16 and 168 registers, three wavefronts a SIMD.
 constexpr int gn_rows(int size, bool backward) { return backward ? (size == 4 ? 4 : 8) : (size == 4 ? 8 : 16); }
 constexpr int GN_STAT_ROWS = 8, GN_APPLY_ROWS = 4;
 constexpr int GN_MOST_GRID = 1 << 20; // workgroups of a launch; they take item after item
@@ -51,7 +51,8 @@ static GnPlan gn_plan(int64_t samples, int64_t pixels, int64_t channels, int64_t
     const int rows = gn_rows(size, backward);
     // Slices from the narrowest on: as wide as 128 bytes, then wider while there are workgroups to spare and threads without a pixel, or none that fit.
     // Of the numbers of threads the first that holds lines of 128 bytes (of 64 where no codes are written), or else the widest of any: workgroups that are small run beside others,
-    // whose loads, sums and stores overlap, but rows in pieces of 32 bytes are slow (512 x 32x32 x 128 bf16 forward 62 us in pieces of 64 bytes, 76 in those of 32).
+    // whose loads, sums and stores overlap, but rows in pieces of 32 bytes are slow (512 x 32x32 x 128 bf16 backward 131 us by 256 threads and 32 bytes, 118 by 512 and 64, 135
+    // by 1024 and 128; with codes written 103 in pieces of 128 bytes, 107 in those of 64).
     const int64_t enough = kept ? 128 : 64;
     GnCut best = {};
     for (int threads : {256, 512, 1024}) {
@@ -72,13 +73,15 @@ static GnPlan gn_plan(int64_t samples, int64_t pixels, int64_t channels, int64_t
         if (most * size >= enough || most >= row) break;
     }
     // Fewer workgroups than compute units: narrower slices, and all the threads there are, for the shortest way through (1 x 32x32 x 128 bf16 9.8 us, by the rule above 13.1).
+    // Forward, samples of a chunk for each of 1024 threads at most stay whole, which spares the launch that adds the goodness of slices (1 x 4x4 x 512 bf16 8.1 us, in slices 9.1,
+    // 64 x 8x8 x 64 7.3 and 9.3; with 2048 chunks alike, with 4096 10.7 and 9.2).
     const int64_t units = 256;
     if (best.slice > 0 && samples * best.slices < units) {
-        int64_t w = std::min(step, row);
+        int64_t w = !backward && pixels * (row / 8) <= 1024 ? row : std::min(step, row);
         while (w < row && samples * ((row + w - 1) / w) > units) w = std::min(w + step, row);
         const int64_t slots = (w + 7) / 8;
         for (int threads : {1024, 512, 256}) {
-            if (w > best.slice || slots > threads || gn_lds(threads, slots, gn_cells(d, backward), d) > GN_MOST_LDS) continue;
+            if ((w > best.slice && w < row) || slots > threads || gn_lds(threads, slots, gn_cells(d, backward), d) > GN_MOST_LDS) continue;
             if (threads > 256 && threads / 2 >= pixels * slots) continue;   // (half of them would do)
             if ((pixels + threads / slots - 1) / (threads / slots) > rows) continue;
             best = {threads, (int32_t)slots, (int32_t)(threads / slots), (int32_t)w, (int32_t)((row + w - 1) / w)};
