@@ -340,6 +340,7 @@ template <typename T, bool RAGGED, bool FROM_X, int CELLS, int ACT> static hipEr
         a.sums = g.dweight || g.dbias ? sums : nullptr;
         a.s = slab_of(p.cut, g.samples, g.pixels, g.channels, g.groups, 1, 8);
         const size_t lds = gn_lds(p.cut.threads, p.cut.slots, 8, d);
+        // slabs of a quarter of the pixels by a kernel of no more (45 x 33x33 x 1 bf16 forward 14.0 us, by the other 18.7; 138 x 5x5 x 23 backward 10.0 and 12.1)
         constexpr int U = gn_rows(sizeof(T), true), FEW = U / 4;
         auto* const kernel = p.cut.lanes * FEW >= g.pixels ? k_gn_backward<T, RAGGED, FROM_X, CELLS, ACT, FEW> : k_gn_backward<T, RAGGED, FROM_X, CELLS, ACT, U>;
         GN_TRY(with_lds(kernel, lds));
