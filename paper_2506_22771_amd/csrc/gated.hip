@@ -40,12 +40,12 @@ __device__ __forceinline__ uint32_t dpp_max8(uint32_t v)
     v = quad_max_u32(v);
     return max(v, dpp_u32<0x141>(v));
 }
-// f(g) u of four places
-template <typename T> __device__ __forceinline__ void gate4(int act, const float g[4], const float u[4], float y[4])
+// f(g) u of N places
+template <typename T, int N> __device__ __forceinline__ void gate(int act, const float (&g)[N], const float (&u)[N], float (&y)[N])
 {
     auto of = [&](auto kind) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < N; ++i) {
             float f, d;
             act_of<T, decltype(kind)::value, true>(g[i], f, d);
             y[i] = f * u[i];
@@ -193,12 +193,12 @@ template <typename T> __global__ __launch_bounds__(WAVES * 64) void k_gated_few(
         // columns beyond the matrix are no part of a block (their sums are zero, but the scale may be anything)
         if (j + e >= a.n) fg[e] = fu[e] = 0.0f;
     }
-    gate4<T>(a.act, fg, fu, y);
+    gate<T>(a.act, fg, fu, y);
     if (i < a.rows && j < a.n) store4((T*)a.y + ((int64_t)i * a.ldy + j), a.n - j, y);
     if (a.good) {
         float s = 0;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s = j + e < a.n ? __builtin_fmaf(y[e], y[e], s) : s;
+        for (int e = 0; e < 4; ++e) s = __builtin_fmaf(y[e], y[e], s);   // (zero beyond the matrix)
         s = dpp_add8(s);
         if ((tid & 7) == 0 && i < a.rows) a.good[(int64_t)bj * a.rows + i] = s;
     }
@@ -251,6 +251,19 @@ __device__ __forceinline__ void tile_of(const GatedTiles& t, int at, int& bi, in
     const int block = at / (8 * t.j), first = block * 8, high = min(8, t.i - first), rest = at - first * t.j;
     bj = rest / high;
     bi = first + (rest - bj * high);
+}
+
+// Bits of the largest magnitude of a lane's and its partner's (32 lanes on) sums, scaled.
+__device__ __forceinline__ uint32_t abs_max16(const v16i& sum, float scale)
+{
+    int hi = sum[0], lo = sum[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) {
+        hi = max(hi, sum[e]);
+        lo = min(lo, sum[e]);
+    }
+    const int m = max(hi, -lo);   // (sums are below 2^31)
+    return __float_as_uint((float)max(m, __shfl_xor(m, 32)) * scale) & 0x7FFFFFFFu;
 }
 
 template <typename T, int BM, int BN, int WM, int WN> __global__ __launch_bounds__(WM* WN * 64) void k_gated_tiles(GatedArgs a, GatedTiles tiles)
@@ -375,13 +388,9 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ __launch_bounds
                 for (int e = 0; e < 16; ++e)
                     if (jw + 8 * (e >> 2) + 4 * lh + (e & 3) >= a.n) g[e] = u[e] = 0.0f;
             if (a.g.q) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    top_g = max(top_g, __float_as_uint(g[e]) & 0x7FFFFFFFu);
-                    top_u = max(top_u, __float_as_uint(u[e]) & 0x7FFFFFFFu);
-                }
-                top_g = max(top_g, (uint32_t)__shfl_xor((int)top_g, 32));
-                top_u = max(top_u, (uint32_t)__shfl_xor((int)top_u, 32));
+                // the largest magnitude is that of the largest sum: rounding and the scale keep their order (an infinite scale leaves no block finite, either way)
+                top_g = abs_max16(acc[ti][0], sc);
+                top_u = abs_max16(acc[ti][1], sc);
                 const uint32_t eg = ckpt_exponent(top_g), eu = ckpt_exponent(top_u);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
@@ -391,14 +400,11 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ __launch_bounds
                 top_g = eg;
                 top_u = eu;
             }
+            gate<T>(a.act, g, u, u);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                float y[4];
-                gate4<T>(a.act, g + 4 * q, u + 4 * q, y);
+            for (int e = 0; e < 16; ++e) good = __builtin_fmaf(u[e], u[e], good);   // (zero beyond the matrix)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) good = !edge || jw + 8 * q + 4 * lh + e < a.n ? __builtin_fmaf(y[e], y[e], good) : good;
-                stage4((T*)(mine + lr * YROW) + 8 * q + 4 * lh, y);
-            }
+            for (int q = 0; q < 4; ++q) stage4((T*)(mine + lr * YROW) + 8 * q + 4 * lh, u + 4 * q);
             good += __shfl_xor(good, 32);
             wave_lds_fence();
             if (prefetched && !waited) {   // copies and stores complete in issue order: before the first store
@@ -506,7 +512,7 @@ template <typename T> __global__ __launch_bounds__(ROW_WAVES * 64) void k_gated_
         g[e] = (float)ag[e] * sc;
         u[e] = (float)au[e] * sc;
     }
-    gate4<T>(a.act, g, u, y);
+    gate<T>(a.act, g, u, y);
     if (l16 < a.rows && j < a.n) store4((T*)a.y + ((int64_t)l16 * a.ldy + j), a.n - j, y);
     if (a.good) {
 #pragma unroll
