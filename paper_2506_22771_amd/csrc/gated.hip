@@ -6,6 +6,7 @@
 // place and neither is ever in memory at more than 8 bits.  Accumulators are exact; g and u are the int32 sums, rounded to fp32, times s.
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "act.hpp"
 #include "blocks.hpp"
@@ -234,11 +235,14 @@ template <int N> __device__ __forceinline__ void wait_copies()   // all but N of
 {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
-// 16 bytes a lane from a buffer straight into LDS at lds_base + lane * 16; completion is tracked by hand
-__device__ __forceinline__ void copy16(__amdgpu_buffer_rsrc_t rsrc, int voffset, int soffset, unsigned lds_base)
+// 16 bytes a lane from a buffer straight into LDS at lds_base + AT + lane * 16; completion is tracked by hand.  (The sum is made where it is used: kept, those of both
+// stages are more scalars than there are.)
+template <int AT> __device__ __forceinline__ void copy16(__amdgpu_buffer_rsrc_t rsrc, int voffset, int soffset, unsigned lds_base)
 {
-    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds_base), "v"(voffset), "s"(rsrc), "s"(soffset) : "memory", "m0");
+    asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(lds_base), "v"(voffset), "s"(rsrc), "s"(soffset), "n"(AT) : "memory", "m0", "scc");
 }
+// each(0), ..., each(N - 1), as constants
+template <typename F, int... I> __device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F&& each) { (each(std::integral_constant<int, I>()), ...); }
 constexpr int BEYOND = 0x7FFFFFF0;   // a byte offset beyond any buffer
 __device__ __forceinline__ int swizzled(int row, int chunk) { return row * 128 + ((chunk ^ ((row >> 1) & 7)) << 4); }
 
@@ -296,13 +300,10 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ __launch_bounds
     auto issue = [&](int kt, int buf) {
         const int k0 = __builtin_amdgcn_readfirstlane(kt * 128);
         const bool in = k0 + kcol < kpad;   // only the last step has chunks beyond the reduction
-        int8_t* const base = lds + buf * STAGE;
-#pragma unroll
-        for (int s = 0; s < CH_P; ++s) copy16(rp, in ? off_p[s] : BEYOND - k0, k0, (unsigned)(uintptr_t)(base + (s * THREADS + wave * 64) * 16));
-#pragma unroll
-        for (int s = 0; s < CH_W; ++s) copy16(rg, in ? off_w[s] : BEYOND - k0, k0, (unsigned)(uintptr_t)(base + BM * 128 + (s * THREADS + wave * 64) * 16));
-#pragma unroll
-        for (int s = 0; s < CH_W; ++s) copy16(ru, in ? off_w[s] : BEYOND - k0, k0, (unsigned)(uintptr_t)(base + (BM + BN) * 128 + (s * THREADS + wave * 64) * 16));
+        const unsigned base = (unsigned)(uintptr_t)(lds + buf * STAGE + wave * 1024);
+        each_of(std::make_integer_sequence<int, CH_P>(), [&](auto s) { copy16<s * THREADS * 16>(rp, in ? off_p[s] : BEYOND - k0, k0, base); });
+        each_of(std::make_integer_sequence<int, CH_W>(), [&](auto s) { copy16<BM * 128 + s * THREADS * 16>(rg, in ? off_w[s] : BEYOND - k0, k0, base); });
+        each_of(std::make_integer_sequence<int, CH_W>(), [&](auto s) { copy16<(BM + BN) * 128 + s * THREADS * 16>(ru, in ? off_w[s] : BEYOND - k0, k0, base); });
     };
     const bool early = wave < WM * WN / 2;
     bool prefetched = false;
