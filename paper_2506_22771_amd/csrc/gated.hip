@@ -228,8 +228,9 @@ template <typename T> __global__ __launch_bounds__(WAVES * 64) void k_gated_few(
 // wavefronts issue a step's copies before its last multiplies and half after them.  A wavefront has the same 32 columns of both projections, which is one
 // checkpoint block: its exponent takes a maximum inside a lane and one exchange.  A workgroup takes tile after tile, the next one's first copies under way
 // during the epilogue; tiles go to an XCD in blocks of eight rows of tiles, which share operands in its L2.
-// 16384 x 4096 x 4096 bf16, kept: 520 to 560 us, 1.10e12 operations at 2.0 to 2.1 POP/s, where a library's int8 product alone takes 558.  The matrix pipe is busy for 53 % of the clocks
-// (beside it, LDS reads take 384 of every 512: six fragments to eight multiplies), and 280 MB of stores are 50 us.
+// 16384 x 4096 x 4096 bf16, kept: 504 to 525 us, 1.10e12 operations at 2.1 to 2.2 POP/s, where a library's int8 product alone takes 558.  The matrix pipe is busy for half of
+// the clocks (beside it, LDS reads take 384 of every 512: six fragments to eight multiplies), and 280 MB of stores are 50 us.  Short reductions are bound by the epilogue:
+// 16384 x 64 x 1024 bf16, kept, 26 us, 68 MB written; 60000 x 128 x 1000 fp32 69 us, 240 MB.
 // ------------------------------------------------------------------------------------------------
 template <int N> __device__ __forceinline__ void wait_copies()   // all but N of this wavefront's copies and stores
 {
@@ -561,9 +562,9 @@ template <typename T, int BM, int BN, int WM, int WN> static void tiles_launch(c
 }
 
 // Which kernel, by what was measured (us; bf16, kept, samples x inputs x outputs; 32 x 32 tiles, 128 x 64, 256 x 128):
-//   up to four 32 x 32 tiles for a compute unit: 512 x 784 x 2000 10.5 11.4 21.7, 256 x 4096 x 4096 22.6 27.9 48.8; twice as many: 1024 x 784 x 2000 17.5 12.7 22.3
+//   up to four 32 x 32 tiles for a compute unit: 512 x 784 x 2000 11.2 10.6 19.8, 256 x 4096 x 4096 24.5 27.6 46.5; twice as many: 1024 x 784 x 2000 18.2 12.0 20.0
 //   beyond, whichever takes fewer rounds of the chip's tiles, one of 256 x 128 counting as 1.75 of 128 x 64, two of which share a compute unit:
-//   2048 x 784 x 2000 31.7 17.3 24.1, 2048 x 4096 x 4096 178 82 69, 4096 x 2000 x 2000 104 49 42, 6000 x 2000 x 2000 148 70 78, 8192 x 2000 x 2000 197 90 82
+//   2048 x 784 x 2000 33 16.6 22.0, 2048 x 4096 x 4096 181 89 72, 4096 x 2000 x 2000 100 46 40, 6000 x 2000 x 2000 142 65 71, 8192 x 2000 x 2000 191 84 73, 16384 x 64 x 1024 65 28 26
 enum GatedKernel { GATED_ROWS, GATED_FEW, GATED_MIDDLE, GATED_LARGE };
 static GatedKernel gated_kernel(int64_t rows, int64_t n, bool kept)
 {
