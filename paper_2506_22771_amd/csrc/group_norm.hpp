@@ -205,9 +205,14 @@ template <typename Args, typename F> static hipError_t launch_items(Args a, F&& 
     return hipSuccess;
 }
 
+// LDS for a kernel's launch.  The plan asks for no more than there is; an error of the runtime is returned here and not kept for the next call to find.
 template <typename F> static hipError_t with_lds(F* kernel, size_t bytes)
 {
-    return bytes <= 65536 ? hipSuccess : hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (bytes <= 65536) return hipSuccess;
+    if (bytes > GN_MOST_LDS) return hipErrorInvalidValue;
+    const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != hipSuccess) (void)hipGetLastError();
+    return e;
 }
 #define GN_TRY(e) do { const hipError_t _e = (e); if (_e != hipSuccess) return _e; } while (0)
 
@@ -218,7 +223,7 @@ template <typename F> static hipError_t by_columns(int64_t channels, int64_t gro
     using Whole = std::false_type;
     using Ragged = std::true_type;
     if (channels % 8 != 0) return launch(Ragged(), Cells<8>());
-    return channels / groups % 4 == 0 ? launch(Whole(), Cells<2>()) : launch(Whole(), Cells<8>());
+    return gn_cells(channels, channels / groups, false) == 2 ? launch(Whole(), Cells<2>()) : launch(Whole(), Cells<8>());
 }
 template <typename F> static hipError_t by_activation(int act, F&& launch)
 {

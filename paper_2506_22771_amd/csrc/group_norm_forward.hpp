@@ -348,7 +348,7 @@ template <typename T, bool RAGGED, GnKept KEPT, int CELLS, int ACT> static hipEr
         a.pieces = p.pieces;
         a.blocks = p.blocks;
         a.rows = p.stat.lanes * GN_STAT_ROWS;
-        const int cells = p.pieces > 1 || RAGGED || p.stat.slice % 8 != 0 ? 8 : gn_cells(d, false);
+        const int cells = p.pieces > 1 || p.stat.slice % 8 != 0 ? 8 : gn_cells(f.channels, d, false);
         a.s = slab_of(p.stat, f.samples, f.pixels, f.channels, f.groups, p.blocks, cells);
         const size_t lds = gn_lds(p.stat.threads, p.stat.slots, cells, d);
         const bool ragged = RAGGED || p.stat.slice % 8 != 0 || (p.pieces > 1 && d % 8 != 0);   // slices that end inside a chunk

@@ -21,8 +21,10 @@ struct GnCut {
     int32_t threads, slots, lanes;   // of a workgroup
     int32_t slice, slices;           // columns of a slice, slices of a row
 };
-// Sums of a chunk that are kept apart: two where its halves lie in one group each, else eight; of columns always eight.
+// Sums of a chunk that are kept apart: two where its halves lie in one group each, else eight; of columns always eight.  Of rows of whole chunks, and of any row, whose
+// kernel has eight where it ends inside a chunk: what the plan counts and what is launched (by_columns).
 static int gn_cells(int64_t d, bool backward) { return !backward && d % 4 == 0 ? 2 : 8; }
+static int gn_cells(int64_t channels, int64_t d, bool backward) { return channels % 8 == 0 ? gn_cells(d, backward) : 8; }
 // threads that share the sum of a cell over the lanes, at most
 static int gn_parts(int threads, int64_t slots, int cells) { return (int)std::max<int64_t>(1, std::min<int64_t>(32, std::min<int64_t>(threads / slots, threads / (slots * cells)))); }
 // LDS of a workgroup: sums of two values per cell, of groups, and a row of weights
@@ -48,7 +50,7 @@ static GnPlan gn_plan(int64_t samples, int64_t pixels, int64_t channels, int64_t
     GnPlan p = {};
     const int64_t d = channels / groups, unit = kept ? 32 : 8, step = d / gn_gcd(d, unit) * unit;
     const int64_t row = gn_up(kept ? span : channels, unit);   // columns of a row with what is behind it
-    const int rows = gn_rows(size, backward);
+    const int rows = gn_rows(size, backward), cells = gn_cells(channels, d, backward);
     // Slices from the narrowest on: as wide as 128 bytes, then wider while there are workgroups to spare and threads without a pixel, or none that fit.
     // Of the numbers of threads the first that holds lines of 128 bytes (of 64 where no codes are written), or else the widest of any: workgroups that are small run beside others,
     // whose loads, sums and stores overlap, but rows in pieces of 32 bytes are slow (512 x 32x32 x 128 bf16 backward 131 us by 256 threads and 32 bytes, 118 by 512 and 64, 135
@@ -59,7 +61,7 @@ static GnPlan gn_plan(int64_t samples, int64_t pixels, int64_t channels, int64_t
         int64_t most = 0;
         for (int64_t w = std::min(step, row);; w = std::min(w + step, row)) {
             const int64_t slots = (w + 7) / 8;
-            if (slots > threads || gn_lds(threads, slots, gn_cells(d, backward), d) > GN_MOST_LDS) break;
+            if (slots > threads || gn_lds(threads, slots, cells, d) > GN_MOST_LDS) break;
             const int64_t lanes = threads / slots, slices = (row + w - 1) / w;
             if ((pixels + lanes - 1) / lanes > rows) break;
             most = w;
@@ -81,7 +83,7 @@ static GnPlan gn_plan(int64_t samples, int64_t pixels, int64_t channels, int64_t
         while (w < row && samples * ((row + w - 1) / w) > units) w = std::min(w + step, row);
         const int64_t slots = (w + 7) / 8;
         for (int threads : {1024, 512, 256}) {
-            if ((w > best.slice && w < row) || slots > threads || gn_lds(threads, slots, gn_cells(d, backward), d) > GN_MOST_LDS) continue;
+            if ((w > best.slice && w < row) || slots > threads || gn_lds(threads, slots, cells, d) > GN_MOST_LDS) continue;
             if (threads > 256 && threads / 2 >= pixels * slots) continue;   // (half of them would do)
             if ((pixels + threads / slots - 1) / (threads / slots) > rows) continue;
             best = {threads, (int32_t)slots, (int32_t)(threads / slots), (int32_t)w, (int32_t)((row + w - 1) / w)};
