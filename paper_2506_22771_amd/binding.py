@@ -156,6 +156,26 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr()
 
 
+def _refuse_type(t: torch.Tensor, of: torch.dtype) -> None:
+    raise ValueError(f"{of} tensor expected, got {t.dtype}")
+
+
+def _typed(*of: torch.dtype):
+    """_ptr for tensors of these types: the library takes what lies at an address for what its header names."""
+    def ptr(t: Optional[torch.Tensor]) -> Optional[int]:
+        if t is None:
+            return None
+        if t.dtype not in of:
+            _refuse_type(t, of[0])
+        if not t.is_cuda or not t.is_contiguous():
+            return _ptr(t)   # (which says so)
+        return t.data_ptr()
+    return ptr
+
+
+_f32, _i8, _i32, _i64 = _typed(torch.float32), _typed(torch.int8), _typed(torch.int32), _typed(torch.int64, torch.uint64)
+
+
 def _stream() -> int:
     if not torch.cuda.is_initialized():
         return torch.cuda.current_stream().cuda_stream
@@ -209,43 +229,43 @@ def ff_layer_workspace_bytes(desc: LayerDesc) -> int:
 
 
 def ff_quantize(x, rows, cols, round_mode, seed, stream_tag, q, q_t, scale, ws) -> None:
-    _chk(lib().ff_quantize(_ptr(x), rows, cols, round_mode, seed, stream_tag, _ptr(q), _ptr(q_t), _ptr(scale),
+    _chk(lib().ff_quantize(_f32(x), rows, cols, round_mode, seed, stream_tag, _i8(q), _i8(q_t), _f32(scale),
                            _ptr(ws), ws.numel() * ws.element_size() if ws is not None else 0, _stream()), "ff_quantize")
 
 
 def ff_layer_forward(desc, a_q, w_q, acc, gsum_int, vmax, ws) -> None:
-    _chk(lib().ff_layer_forward(C.byref(desc), _ptr(a_q), _ptr(w_q), _ptr(acc), _ptr(gsum_int), _ptr(vmax), _ptr(ws),
+    _chk(lib().ff_layer_forward(C.byref(desc), _i8(a_q), _i8(w_q), _i32(acc), _i64(gsum_int), _i32(vmax), _ptr(ws),
                                 ws.numel() * ws.element_size() if ws is not None else 0, _stream()), "ff_layer_forward")
 
 
 def ff_goodness_loss(desc, gsum_int, vmax, s_a, s_w, pass_sign, theta, goodness, coeff, loss_mean, next_amax) -> None:
-    _chk(lib().ff_goodness_loss(C.byref(desc), _ptr(gsum_int), _ptr(vmax), _ptr(s_a), _ptr(s_w), pass_sign, theta,
-                                _ptr(goodness), _ptr(coeff), _ptr(loss_mean), _ptr(next_amax), _stream()),
+    _chk(lib().ff_goodness_loss(C.byref(desc), _i64(gsum_int), _i32(vmax), _f32(s_a), _f32(s_w), pass_sign, theta,
+                                _f32(goodness), _f32(coeff), _f32(loss_mean), _f32(next_amax), _stream()),
          "ff_goodness_loss")
 
 
 def ff_layer_handoff(desc, acc, s_a, s_w, goodness, amax, round_mode, seed, stream_tag, q, q_t, scale) -> None:
-    _chk(lib().ff_layer_handoff(C.byref(desc), _ptr(acc), _ptr(s_a), _ptr(s_w), _ptr(goodness), _ptr(amax), round_mode,
-                                seed, stream_tag, _ptr(q), _ptr(q_t), _ptr(scale), _stream()), "ff_layer_handoff")
+    _chk(lib().ff_layer_handoff(C.byref(desc), _i32(acc), _f32(s_a), _f32(s_w), _f32(goodness), _f32(amax), round_mode,
+                                seed, stream_tag, _i8(q), _i8(q_t), _f32(scale), _stream()), "ff_layer_handoff")
 
 
 def ff_lookahead(coeff, n_layers, batch, lam, coeff_total) -> None:
-    _chk(lib().ff_lookahead(_ptr(coeff), n_layers, batch, lam, _ptr(coeff_total), _stream()), "ff_lookahead")
+    _chk(lib().ff_lookahead(_f32(coeff), n_layers, batch, lam, _f32(coeff_total), _stream()), "ff_lookahead")
 
 
 def ff_layer_backward_local(desc, acc, vmax, s_a, s_w, coeff_total, round_mode, seed, stream_tag, a_q_t, gy_q_t, s_g,
                             dw_acc, ws) -> None:
-    _chk(lib().ff_layer_backward_local(C.byref(desc), _ptr(acc), _ptr(vmax), _ptr(s_a), _ptr(s_w), _ptr(coeff_total),
-                                       round_mode, seed, stream_tag, _ptr(a_q_t), _ptr(gy_q_t), _ptr(s_g), _ptr(dw_acc),
+    _chk(lib().ff_layer_backward_local(C.byref(desc), _i32(acc), _i32(vmax), _f32(s_a), _f32(s_w), _f32(coeff_total),
+                                       round_mode, seed, stream_tag, _i8(a_q_t), _i8(gy_q_t), _f32(s_g), _i32(dw_acc),
                                        _ptr(ws), ws.numel() * ws.element_size() if ws is not None else 0, _stream()),
          "ff_layer_backward_local")
 
 
 def ff_layer_backward_local_noalloc(desc, acc, vmax, s_a, s_w, coeff_total, round_mode, seed, stream_tag, a_q_t,
                                     gy_q_t, s_g, dw_acc) -> None:
-    _chk(lib().ff_layer_backward_local_noalloc(C.byref(desc), _ptr(acc), _ptr(vmax), _ptr(s_a), _ptr(s_w),
-                                               _ptr(coeff_total), round_mode, seed, stream_tag, _ptr(a_q_t),
-                                               _ptr(gy_q_t), _ptr(s_g), _ptr(dw_acc), _stream()),
+    _chk(lib().ff_layer_backward_local_noalloc(C.byref(desc), _i32(acc), _i32(vmax), _f32(s_a), _f32(s_w),
+                                               _f32(coeff_total), round_mode, seed, stream_tag, _i8(a_q_t),
+                                               _i8(gy_q_t), _f32(s_g), _i32(dw_acc), _stream()),
          "ff_layer_backward_local_noalloc")
 
 
@@ -254,21 +274,21 @@ def ff_noalloc_scratch_bytes() -> int:
 
 
 def ff_chain_gradients(desc, acc, s_a, s_w, coeff, e_acc, s_h, s_w_up, lam, h, g, h_amax, g_amax) -> None:
-    _chk(lib().ff_chain_gradients(C.byref(desc), _ptr(acc), _ptr(s_a), _ptr(s_w), _ptr(coeff), _ptr(e_acc), _ptr(s_h),
-                                  _ptr(s_w_up), lam, _ptr(h), _ptr(g), _ptr(h_amax), _ptr(g_amax), _stream()),
+    _chk(lib().ff_chain_gradients(C.byref(desc), _i32(acc), _f32(s_a), _f32(s_w), _f32(coeff), _i32(e_acc), _f32(s_h),
+                                  _f32(s_w_up), lam, _f32(h), _f32(g), _f32(h_amax), _f32(g_amax), _stream()),
          "ff_chain_gradients")
 
 
 def ff_layer_input_grad(desc, h_q, w_q_t, e_acc, ws) -> None:
-    _chk(lib().ff_layer_input_grad(C.byref(desc), _ptr(h_q), _ptr(w_q_t), _ptr(e_acc), _ptr(ws),
+    _chk(lib().ff_layer_input_grad(C.byref(desc), _i8(h_q), _i8(w_q_t), _i32(e_acc), _ptr(ws),
                                    ws.numel() * ws.element_size() if ws is not None else 0, _stream()),
          "ff_layer_input_grad")
 
 
 def ff_layer_update(desc, w_master, dw_pos, s_g_pos, s_a_pos, dw_neg, s_g_neg, s_a_neg, lr, total_samples, w_q, s_w,
                     ws) -> None:
-    _chk(lib().ff_layer_update(C.byref(desc), _ptr(w_master), _ptr(dw_pos), _ptr(s_g_pos), _ptr(s_a_pos), _ptr(dw_neg),
-                               _ptr(s_g_neg), _ptr(s_a_neg), lr, total_samples, _ptr(w_q), _ptr(s_w), _ptr(ws),
+    _chk(lib().ff_layer_update(C.byref(desc), _f32(w_master), _i32(dw_pos), _f32(s_g_pos), _f32(s_a_pos), _i32(dw_neg),
+                               _f32(s_g_neg), _f32(s_a_neg), lr, total_samples, _i8(w_q), _f32(s_w), _ptr(ws),
                                ws.numel() * ws.element_size() if ws is not None else 0, _stream()), "ff_layer_update")
 
 
@@ -289,6 +309,10 @@ class Net:
         self.desc = NetDesc(self.k, batch, self._descs, self._mask, {"coeff": 0, "chain": 1}[lookahead], self._theta,
                             {"auto": 0, "kernels": 1, "fused": 2, "lanes": 3}[launch_mode])
         self.w_master, self.w_q, self.s_w = list(w_master), list(w_q), list(s_w)
+        for of, tensors in ((torch.float32, self.w_master), (torch.int8, self.w_q), (torch.float32, self.s_w)):
+            for t in tensors:
+                if t.dtype is not of:
+                    _refuse_type(t, of)
         self._pm = (C.c_void_p * self.k)(*[t.data_ptr() for t in self.w_master])
         self._pq = (C.c_void_p * self.k)(*[t.data_ptr() for t in self.w_q])
         self._ps = (C.c_void_p * self.k)(*[t.data_ptr() for t in self.s_w])
@@ -303,14 +327,14 @@ def ff_workspace_bytes(net: Net) -> int:
 
 
 def ff_train_step(net: Net, x_pos, x_neg, theta, lam, lr, seed, step, loss, goodness, ws) -> None:
-    _chk(lib().ff_train_step(C.byref(net.desc), C.byref(net.state), _ptr(x_pos), _ptr(x_neg), theta, lam, lr, seed,
-                             step, _ptr(loss), _ptr(goodness), _ptr(ws),
+    _chk(lib().ff_train_step(C.byref(net.desc), C.byref(net.state), _f32(x_pos), _f32(x_neg), theta, lam, lr, seed,
+                             step, _f32(loss), _f32(goodness), _ptr(ws),
                              ws.numel() * ws.element_size() if ws is not None else 0, _stream()), "ff_train_step")
 
 
 def ff_train_step_at(net: Net, x_pos, x_neg, theta, lam, lr, seed, step_dev, advance, loss, goodness, ws) -> None:
-    _chk(lib().ff_train_step_at(C.byref(net.desc), C.byref(net.state), _ptr(x_pos), _ptr(x_neg), theta, lam, lr, seed,
-                                _ptr(step_dev), int(advance), _ptr(loss), _ptr(goodness), _ptr(ws),
+    _chk(lib().ff_train_step_at(C.byref(net.desc), C.byref(net.state), _f32(x_pos), _f32(x_neg), theta, lam, lr, seed,
+                                _i64(step_dev), int(advance), _f32(loss), _f32(goodness), _ptr(ws),
                                 ws.numel() * ws.element_size() if ws is not None else 0, _stream()), "ff_train_step_at")
 
 
