@@ -6,13 +6,16 @@
 namespace ffi {
 
 // f(u) and f'(u).  GELU's exponential is the density's as well as a factor of Phi(-|u|).
-// 16-bit values: Phi(-|u|) = 1/2 t (a1 + t (a2 + ...)) exp(-u^2/2), t = 1 / (1 + p |u| / sqrt 2): Abramowitz and Stegun 7.1.26, off by at most 0.75e-7, far
-// below their rounding of 2^-9 or 2^-12.  With more arithmetic than this the large case is bound by it and not by memory: 16384 x 4096 bf16 values 96 us with
+// 16-bit values, where f' is the output (not ANY): Phi(-|u|) = 1/2 t (a1 + t (a2 + ...)) exp(-u^2/2), t = 1 / (1 + p |u| / sqrt 2): Abramowitz and Stegun 7.1.26, off by at
+// most 0.75e-7, and f' by no more than that.  With more arithmetic than this the large case is bound by it and not by memory: 16384 x 4096 bf16 values 96 us with
 // the library's erf and exp, 62 to 65 this way.
+// 16-bit values, where f is an output too (ANY): far below zero f = u Phi(u) is as small as Phi, of which that sum is off by 6e-4 at u = -4.2 and 4e-3 at -6, more than half
+// a step of fp16 and of bf16.  One term more, fitted to errors relative to Phi as well: off by at most 1.1e-8, and by 2.8e-5 of Phi down to -6, 6e-4 down to -9.  (rms of
+// fp32 outputs: f' 6.1e-8 of its size, by the shorter sum 9.9e-8.)
 // fp32 values: that is more than the rounding of an fp32 product (rms of f' 9.7e-8 of its size), so Phi = 1/2 + u P(u^2) up to |u| = 1.25, off by at most 2.1e-9, and
 // Phi(-|u|) = t Q(t) exp(-u^2/2), t = 1 / (1 + 0.3 |u|), beyond, off by at most 4.3e-9; P and Q are least-squares fits, reweighted towards the smallest largest
 // error (rms of f' 4.0e-8; with the device library's erf 4.1e-8, and 16384 x 4096 values with goodness 114 us, 120 that way, 109 by the sum above and with ReLU).
-// ANY: of any fp32 argument; else of what a checkpoint holds.
+// ANY: of any fp32 argument, with f as an output; else of what a checkpoint holds, for the gradient.
 template <typename T, int ACT, bool ANY = false> __device__ __forceinline__ void act_of(float u, float& f, float& d)
 {
     if constexpr (ACT == FF_ACT_RELU) {
@@ -34,6 +37,15 @@ template <typename T, int ACT, bool ANY = false> __device__ __forceinline__ void
             q = __builtin_fmaf(t, q, 0.11132239f);
             const float low = t * q * e;
             phi = __builtin_fabsf(u) < 1.25f ? __builtin_fmaf(u, p, 0.5f) : u > 0 ? 1.0f - low : low;
+        } else if constexpr (ANY) {
+            const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(u), 0.281f, 1.0f));
+            float q = __builtin_fmaf(t, -0.103819676f, 0.377323121f);
+            q = __builtin_fmaf(t, q, -0.218507633f);
+            q = __builtin_fmaf(t, q, 0.256346375f);
+            q = __builtin_fmaf(t, q, 0.0723568052f);
+            q = __builtin_fmaf(t, q, 0.116301f);
+            const float low = t * q * e;
+            phi = u > 0 ? 1.0f - low : low;
         } else {
             const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_fabsf(u), 0.23164189110f, 1.0f));   // p / sqrt 2
             float q = __builtin_fmaf(t, 0.5307027145f, -0.7265760135f);                     // half of the polynomial
@@ -41,8 +53,7 @@ template <typename T, int ACT, bool ANY = false> __device__ __forceinline__ void
             q = __builtin_fmaf(t, q, -0.142248368f);
             q = __builtin_fmaf(t, q, 0.127414796f);
             // Phi(u): 1 - low above zero, else low; a code that is not zero stands for 2^-106 at least
-            if constexpr (ANY) phi = u > 0 ? 1.0f - t * q * e : t * q * e;
-            else phi = __builtin_fabsf(__builtin_amdgcn_fmed3f(u * 0x1p127f, 0.0f, 1.0f) - t * q * e);
+            phi = __builtin_fabsf(__builtin_amdgcn_fmed3f(u * 0x1p127f, 0.0f, 1.0f) - t * q * e);
         }
         f = u * phi;
         d = __builtin_fmaf(u * e, 0.39894228040143268f, phi);

@@ -59,7 +59,7 @@ template <typename T, int ACT, RowEnds ENDS, int U> __global__ __launch_bounds__
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             float f, d;
-            act_of<T, ACT>(g[j], f, d);
+            act_of<T, ACT, true>(g[j], f, d);
             if (a.coeff) t[j] = __builtin_fmaf(c2, f * u[j], t[j]);   // (uniform)
             g[j] = t[j] * u[j] * d;
             u[j] = t[j] * f;
