@@ -15,6 +15,8 @@ namespace ffi {
 // fp32 values: that is more than the rounding of an fp32 product (rms of f' 9.7e-8 of its size), so Phi = 1/2 + u P(u^2) up to |u| = 1.25, off by at most 2.1e-9, and
 // Phi(-|u|) = t Q(t) exp(-u^2/2), t = 1 / (1 + 0.3 |u|), beyond, off by at most 4.3e-9; P and Q are least-squares fits, reweighted towards the smallest largest
 // error (rms of f' 4.0e-8; with the device library's erf 4.1e-8, and 16384 x 4096 values with goodness 114 us, 120 that way, 109 by the sum above and with ReLU).
+// SiLU of fp32 values (ANY): the exponential's argument x = -u log2(e) is a rounded product, whose error grows with it (f off by 1.7e-6 of itself at u = -60).  What the rounding
+// left, c = -u - x ln 2, goes into it as exp(-u) = 2^x (1 + c).
 // ANY: of any fp32 argument, with f as an output; else of what a checkpoint holds, for the gradient.
 template <typename T, int ACT, bool ANY = false> __device__ __forceinline__ void act_of(float u, float& f, float& d)
 {
@@ -58,7 +60,15 @@ template <typename T, int ACT, bool ANY = false> __device__ __forceinline__ void
         f = u * phi;
         d = __builtin_fmaf(u * e, 0.39894228040143268f, phi);
     } else if constexpr (ACT == FF_ACT_SILU) {
-        const float sig = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(u * -1.4426950408889634f));
+        float e;
+        if constexpr (ANY && sizeof(T) == 4) {
+            const float v = __builtin_amdgcn_fmed3f(u, -88.72283f, 88.72283f), x = v * -1.4426950408889634f;   // (e is finite; beyond, sigma is 0 or 1)
+            e = __builtin_amdgcn_exp2f(x);
+            e = __builtin_fmaf(e, __builtin_fmaf(x, -0.693147182f, -v), e);
+        } else {
+            e = __builtin_amdgcn_exp2f(u * -1.4426950408889634f);
+        }
+        const float sig = __builtin_amdgcn_rcpf(1.0f + e);
         f = u * sig;
         d = __builtin_fmaf(f, 1.0f - sig, sig);
     } else {

@@ -64,6 +64,15 @@ def test_gelu_of_16_bits(dtype, route):
     within(got, ref, np.abs(ref) * (off + HALF_ULP[dtype] * (1 + off)) + TINY[dtype] / size, f"{dtype} {route}")
 
 
+# fp32 SiLU: exp2 and rcp a unit (2 U) each; the exponential's second factor, its sum with one, f = u sigma and f times the value half a unit (U) each.  The argument's rounding is put right to
+# below 2^-40, but for the last place of ln 2 in it: 1.91e-9 of |x| = 1.4427 |u|, 0.047 U for each of |u|.  Where sigma is a normal number.
+@pytest.mark.parametrize("route", list(ROUTES))
+def test_silu_of_32_bits(route):
+    u, got, _ = ROUTES[route]("silu", "float32", 86.0)
+    ref, _ = N.act("silu", u)
+    within(got, ref, np.abs(ref) * (8 + 0.047 * np.abs(u)) * U, route)
+
+
 @pytest.mark.parametrize("dtype", list(DTYPES))
 @pytest.mark.parametrize("kind", ["gelu", "silu"])
 def test_the_largest_arguments(kind, dtype):
