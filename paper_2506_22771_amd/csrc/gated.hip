@@ -454,8 +454,12 @@ template <typename T, int BM, int BN, int WM, int WN> __global__ __launch_bounds
             }
             wave_lds_fence();   // (the next rows' values go where these lie)
         }
-        // every wavefront has waited for its copies of the next tile's first step: they are there for all behind this barrier
-        if (prefetched) __builtin_amdgcn_s_barrier();
+        // Every wavefront has waited for its copies of the next tile's first step: they are there for all behind this barrier.  And for what it staged, also where it has no
+        // columns or rows to read back: the next tile's second step goes where that lies.
+        if (prefetched) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+        }
     }
 }
 
