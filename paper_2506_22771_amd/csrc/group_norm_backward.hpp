@@ -91,7 +91,7 @@ __device__ __forceinline__ void dz_of(const GnPixel<T, FROM_X>& v, const GnGradC
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         float f, d;
-        act_of<T, ACT, true>(__builtin_fmaf(h[i], p.w[i], p.b[i]), f, d);
+        act_of<T, ACT, true, false>(__builtin_fmaf(h[i], p.w[i], p.b[i]), f, d);
         dz[i] = __builtin_fmaf(p.c2, f, dz[i]) * d;
         if (i & 1) one_pixel_at_a_time();
     }
