@@ -531,6 +531,7 @@ ff_status ff_group_norm_forward(int64_t samples, int64_t pixels, int64_t channel
  *   h comes from x, mean and rstd, as (x - mean) * rstd in fp32, or, with x == NULL, from the checkpoint q, e (mean is not read then).
  *   dy or coeff (fp32 [samples]) may be NULL, not both.  dx of type dtype, dweight and dbias fp32 [channels]: any may be NULL, not all three.
  *   dx may be dy or x.  accumulate: 1 adds to dweight and dbias, 0 overwrites them.  ws as above.  samples == 0: sums are zero.
+ *   dweight and dbias are added over the samples in 64 bits.
  * Sums are formed in a fixed order: equal calls give equal bits. */
 ff_status ff_group_norm_backward(int64_t samples, int64_t pixels, int64_t channels, int64_t groups, int32_t dtype, int32_t param_dtype, const void* dy,
                                  int64_t lddy, const float* coeff, const void* x, int64_t ldx, const float* mean, const int8_t* q, const uint8_t* e,
@@ -540,7 +541,7 @@ ff_status ff_group_norm_backward(int64_t samples, int64_t pixels, int64_t channe
 /* ff_dropout — y = r + (u >= p ? x / (1 - p) : 0), u the uniform of element row*cols+col under (seed, stream_tag): the random word of ff_quantize, of
  * which no mask is kept.  The backward pass is the same call on the gradient, without r.
  *   r        [rows, cols], added (may be NULL); y may be x or r
- *   p        0 <= p <= 1; p == 1 drops everything.  What is dropped is zero whatever it was.
+ *   p        0 <= p <= 1, as fp32 holds it, in the comparison and in the scale; p == 1 drops everything.  What is dropped is zero whatever it was.
  *   step_dev one uint64 in DEVICE memory (8-byte aligned) or NULL: the tag is stream_tag + (*step_dev << 20), that of step *step_dev where stream_tag is
  *            ff_stream_tag(0, ...).  Read when the kernel runs: a captured call drops other elements at every replay that has advanced it. */
 ff_status ff_dropout(int64_t rows, int64_t cols, int32_t dtype, const void* x, int64_t ldx, const void* r, int64_t ldr, float p, uint64_t seed,

@@ -2,7 +2,7 @@
 
 Functions mirror the C-ABI names.  Tensor arguments are torch CUDA tensors (or None where the
 header allows NULL); their data_ptr() is handed to the library together with the current
-torch stream.  The calls on matrices of floating-point values (norms, checkpoints, gated layers, dropout) take the compiled way (csrc/bind.cpp).  Nothing here computes."""
+torch stream, its type compared with the header's.  The calls on matrices of floating-point values (norms, checkpoints, gated layers, dropout) take the compiled way (csrc/bind.cpp).  Nothing here computes."""
 from __future__ import annotations
 
 import ctypes as C
@@ -427,7 +427,7 @@ def ff_group_norm_forward(x, samples, groups, weight, bias, eps, act, y, mean, r
 
 
 def ff_group_norm_backward(dy, coeff, x, mean, q, e, rstd, samples, groups, weight, bias, act, dx, dweight, dbias, accumulate, ws) -> None:
-    """h comes from x, mean and rstd, or, with x = None, from the checkpoint q, e and rstd."""
+    """h comes from x, mean and rstd, or, with x = None, from the checkpoint q, e and rstd.  One of dy, x and dx is given: it says how many rows there are, and their type."""
     _chk(_native().group_norm_backward(dy, coeff, x, mean, q, e, rstd, samples, groups, weight, bias, act, dx, dweight, dbias, accumulate, ws, _stream()),
          "ff_group_norm_backward")
 

@@ -2,7 +2,8 @@
 
     python -m paper_2506_22771_amd.build [--force]
 
-and _bind.so, the compiled marshalling of Python's layer norm and checkpoint calls (host code, against Python's and torch's headers), with g++.
+and _bind.so, the compiled marshalling of Python's calls on matrices of floating-point values: norms, checkpoints, gated layers, dropout (host code, against Python's and torch's
+headers), with g++.
 Where one of these is not there the library is built all the same, for its C interface and the other Python calls; what is missing is printed.
 
 -ffp-contract=off: the numerics need one rounding per written fp32 operation (hipcc would fuse).
@@ -64,7 +65,7 @@ def _build_bind(force: bool) -> None:
     if missing:
         if os.path.exists(BIND):
             os.remove(BIND)     # (it is older than the library)
-        print(f"_bind.so is not built ({', '.join(missing)} not found): no layer norm and checkpoint calls from Python", file=sys.stderr)
+        print(f"_bind.so is not built ({', '.join(missing)} not found): no calls of norms, checkpoints, gated layers and dropout from Python", file=sys.stderr)
         return
     torch = needs["torch's headers"]
     subprocess.run([needs["g++"], "-O2", "-fPIC", "-shared", "-std=c++17", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=1", "-I" + torch, "-I" + os.path.join(torch, "torch", "csrc", "api", "include"),

@@ -228,7 +228,7 @@ template <typename T> __global__ __launch_bounds__(WAVES * 64) void k_gated_few(
 // wavefronts issue a step's copies before its last multiplies and half after them.  A wavefront has the same 32 columns of both projections, which is one
 // checkpoint block: its exponent takes a maximum inside a lane and one exchange.  A workgroup takes tile after tile, the next one's first copies under way
 // during the epilogue; tiles go to an XCD in blocks of eight rows of tiles, which share operands in its L2.
-// 16384 x 4096 x 4096 bf16, kept: 504 to 525 us, 1.10e12 operations at 2.1 to 2.2 POP/s, where a library's int8 product alone takes 558.  The matrix pipe is busy for half of
+// 16384 x 4096 x 4096 bf16, kept: 504 to 525 us, 1.10e12 operations at 2.1 to 2.2 POP/s (602 to 606 where the clock falls under the load: box by box, and under a profiler), where a library's int8 product alone takes 558.  The matrix pipe is busy for half of
 // the clocks (beside it, LDS reads take 384 of every 512: six fragments to eight multiplies), and 280 MB of stores are 50 us.  Short reductions are bound by the epilogue:
 // 16384 x 64 x 1024 bf16, kept, 26 us, 68 MB written; 60000 x 128 x 1000 fp32 69 us, 240 MB.
 // ------------------------------------------------------------------------------------------------

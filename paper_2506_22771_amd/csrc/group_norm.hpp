@@ -5,7 +5,7 @@
 //   dz = (dy + 2 c f(z)) f'(z),  dgamma = sum over pixels and samples of dz h,  dbeta = sum of dz
 //   dx = rstd (g - 1/(P d) sum over the group of g - h 1/(P d) sum over the group of g h),  g = gamma dz
 //
-// Statistics, products and sums are fp32 (the means of parts of a group are joined in 64 bits); y and dx are rounded once.  As in the layer norm, the mean of
+// Statistics, products and sums are fp32 (the means of parts of a group, and dgamma and dbeta over the samples, are joined in 64 bits); y and dx are rounded once.  As in the layer norm, the mean of
 // the deviations is taken out of groups farther from zero than they are wide (norm_math.hpp).
 //
 // Memory bounds all of it.  A workgroup's threads lie over a slab of whole groups: a chunk of eight columns is a thread's own from pixel to pixel, so that

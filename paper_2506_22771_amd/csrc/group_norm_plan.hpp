@@ -14,7 +14,7 @@ constexpr int GN_SPLIT_THREADS = 256;
 // beside the sums.  512 x 32x32 x 128 bf16 forward 62 us with 16 and 72 with 8, backward from codes 111 with 8 and 124 with 16 and 168 registers, three wavefronts a SIMD.
 constexpr int gn_rows(int size, bool backward) { return backward ? (size == 4 ? 4 : 8) : (size == 4 ? 8 : 16); }
 constexpr int GN_STAT_ROWS = 8, GN_APPLY_ROWS = 4;
-constexpr int GN_MOST_GRID = 1 << 20; // workgroups of a launch; they take item after item
+constexpr int GN_MOST_GRID = 1 << 20; // workgroups of a launch, one item each: more items are further launches (launch_items).  Those of the joins take item after item
 constexpr size_t GN_MOST_LDS = 150 * 1024;
 
 struct GnCut {
